@@ -116,11 +116,11 @@ def gather_ceiling(gb: float, lines: int) -> None:
 
 
 def kernel_source_hash() -> str:
-    """The library's build id for the sources in this tree (sha256 over the
-    sources without comments and spacing, and the build flags); a committed
-    traffic or parity figure is valid only for the code it was measured on."""
-    from paper_2603_14002_amd.build import source_hash
-    return source_hash()
+    """The decoder's part of the library's sources in this tree (sha256 over them
+    without comments and spacing, and the build flags); a committed traffic or
+    parity figure is valid only for the code it was measured on."""
+    from paper_2603_14002_amd.build import decoder_hash
+    return decoder_hash()
 
 
 def measured_traffic(workload: str):

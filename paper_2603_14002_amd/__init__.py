@@ -16,6 +16,11 @@ from typing import Optional
 
 import numpy as np
 
+from .scorer import (LB_BF16, LB_F16, LB_F32, LB_KV_BAD_LENGTH, LB_KV_BAD_PAGE, LB_MAX_RULE_IDS,  # noqa: F401
+                     LB_ROPE_BLEND, LB_ROPE_HALF, LB_ROPE_INTERLEAVED, LB_ROPE_LINEAR, LB_ROPE_PLAIN, SCORER_EXPORTED,
+                     KVBatch, KVCache, LogitRules, Rope, declare, lb_kv_append, lb_kv_attend, lb_kv_attend_workspace,
+                     lb_kv_read, lb_logits_adjust, lb_logits_workspace, lb_lora_add, lb_lora_workspace, lb_rope_table)
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblightbeam.so")
 
@@ -121,6 +126,7 @@ def lib():
         L.lb_set_profiling.argtypes = [P, ctypes.c_uint32]
         L.lb_last_error.restype = ctypes.c_char_p
         L.lb_last_error.argtypes = []
+        declare(L)
         _lib = L
     return _lib
 

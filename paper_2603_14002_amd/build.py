@@ -13,7 +13,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblightbeam.so")
-SOURCES = ["lb_kernels.hip", "lb_api.cpp"]
+SOURCES = ["lb_kernels.hip", "lb_api.cpp", "lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer_api.cpp"]
 # k_decode loops over frames: machine-level hoisting of loop-invariant values
 # out of that loop keeps them live across it and makes the kernel spill
 EXTRA = {"lb_kernels.hip": ["-mllvm", "-disable-machine-licm"]}
@@ -27,19 +27,34 @@ COMMON = [
 ]
 
 
-# every file whose text goes into the library, for its build id
-HASHED = [os.path.join(CSRC, f) for f in ("lb_kernels.hip", "lb_device.h", "lb_launch.h", "lb_api.cpp")] + \
-    [os.path.join(os.path.dirname(HERE), "include", "lightbeam.h")]
+# every file whose text goes into the library, for its build id: the decoder's, and the scorer operators'
+INCLUDE = os.path.join(os.path.dirname(HERE), "include")
+DECODER = [os.path.join(CSRC, f) for f in ("lb_kernels.hip", "lb_device.h", "lb_launch.h", "lb_api.cpp")] + \
+    [os.path.join(INCLUDE, "lightbeam.h")]
+HASHED = DECODER + [os.path.join(CSRC, f) for f in ("lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer.h",
+                                                    "lb_scorer_api.cpp")] + \
+    [os.path.join(INCLUDE, "lightbeam_scorer.h")]
 
 
 def source_hash() -> str:
-    """sha256 over the library's sources with comments and spacing removed, and
-    over the build flags: the build id compiled into liblightbeam.so, and the
-    id that the binding expects of a library built from this tree."""
+    """The build id compiled into liblightbeam.so, and the id that the binding
+    expects of a library built from this tree."""
+    return _hash(HASHED)
+
+
+def decoder_hash() -> str:
+    """The same over the decoder's files alone: what figures measured on the
+    decoder are good for."""
+    return _hash(DECODER)
+
+
+def _hash(files) -> str:
+    """sha256 over sources with comments and spacing removed, and over the build
+    flags."""
     import hashlib
     import re
     h = hashlib.sha256()
-    for f in HASHED:
+    for f in files:
         with open(f) as fh:
             text = fh.read()
         text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)
