@@ -425,6 +425,10 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t codes, float s) {
                __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
 }
 
+// the larger of two, of a NaN and a number the number (fmaxf would first quiet
+// each operand in an instruction of its own)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, __builtin_inff()); }
+
 // the maximum (sum) over the four lanes of a query row
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -435,161 +439,188 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// One half (16 tokens) of a tile in the cache's form.
+// 255 in each byte that is 255, else 0
+__device__ __forceinline__ uint32_t bytes_255(uint32_t w) {
+  const uint32_t all = (w & 0x7F7F7F7Fu) + 0x01010101u & w & 0x80808080u;  // bit 7: the low seven bits carry into it, and it is set
+  return (all >> 7) * 255u;
+}
+
+// A tile (32 tokens) in the cache's form, by halves of 16 tokens.
 template <int D>
-struct Half {
-  uint32_t k[D / 32];  // D/4 codes: the lane's quarter of key n
-  uint32_t v[D / 32];  // values of tokens 4 j .. 4 j + 3, channel pairs D/32 n .. D/32 (n + 1) - 1
-  uint32_t ks;         // scale bytes of the quarter's blocks (one, or two with D = 256)
-  uint32_t vs;         // scale bytes of the four tokens' values
-  bool ok;             // the page exists
+struct Tile {
+  uint32_t k[2][D / 32];  // D/4 codes: the lane's quarter of key n
+  uint32_t v[2][D / 32];  // values of tokens 4 j .. 4 j + 3, channel pairs D/32 n .. D/32 (n + 1) - 1
+  uint32_t ks[2];         // scale bytes of the quarter's blocks (one, or two with D = 256)
+  uint32_t vs[2];         // scale bytes of the four tokens' values
 };
 
+// The key range of a wavefront: tiles of 32 tokens from `begin` on, every
+// `step`-th of them.  Lane i holds the pages of the i-th of the next 64 tiles, so
+// a tile's address needs no load before it.
 template <int D>
-__device__ __forceinline__ void load_half(const KvArgs& A, int32_t s, int32_t h, int32_t t0, int32_t end, int n, int j, Half<D>& H) {
-  const int64_t page = t0 < end ? page_of(A, s, t0) : -2;
-  H.ok = page >= 0;
-  if (!H.ok) {
-    if (page == -1) raise(A.flags, LB_KV_BAD_PAGE);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) H.k[i] = H.v[i] = 0;
-    H.ks = H.vs = 0;
-    return;
+struct Keys {
+  const uint8_t* base;   // head h of page 0
+  int64_t page_bytes;
+  const int32_t* table;
+  int32_t n_pages, shift, begin, end, step;
+  static constexpr int32_t kNothing = -(1 << 29);  // no tile is within 64 steps of it
+  int32_t held, page0, page1;
+  uint32_t k_at, v_at, ks_at, vs_at;
+
+  __device__ __forceinline__ Keys(const KvArgs& A, int32_t s, int32_t h, int32_t begin_, int32_t end_, int32_t step_, int n, int j)
+      : table(A.table + static_cast<int64_t>(s) * A.max_pages), n_pages(static_cast<int32_t>(A.n_pages)), shift(A.page_shift),
+        begin(begin_), end(end_), step(step_), held(kNothing), page0(-1), page1(-1) {
+    const int32_t P = 1 << shift, block = P * (D + D / 16);
+    base = A.pages + static_cast<int64_t>(h) * block;
+    page_bytes = static_cast<int64_t>(block) * A.kv_heads;
+    k_at = n * (D / 2) + j * (D / 8);
+    v_at = P * (D / 2) + j * (D * 2) + n * (D / 8);
+    ks_at = P * D + n * (D / 32) + j * D / 128;
+    vs_at = P * D + P * (D / 32) + (j * (D / 32) + n * D / 512) * 4;
   }
-  const int32_t P = 1 << A.page_shift, slot = t0 & (P - 1);
-  const uint8_t* block = A.pages + (page * A.kv_heads + h) * (static_cast<int64_t>(P) * (D + D / 16));
-  const uint8_t* k = block + (slot + n) * (D / 2) + j * (D / 8);
-  const uint8_t* v = block + P * D / 2 + (((slot >> 2) + j) * (D / 2) + n * (D / 32)) * 4;
-  if constexpr (D == 64) {
-    const u32x2 a = *reinterpret_cast<const u32x2*>(k), b = *reinterpret_cast<const u32x2*>(v);
-    H.k[0] = a.x, H.k[1] = a.y, H.v[0] = b.x, H.v[1] = b.y;
-  } else {
-#pragma unroll
-    for (int i = 0; i < D / 128; ++i) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(k + 16 * i), b = *reinterpret_cast<const u32x4*>(v + 16 * i);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) H.k[4 * i + x] = a[x], H.v[4 * i + x] = b[x];
+
+  // makes lane i hold the pages of tile t + i * step, if tile `t` has left what is held
+  __device__ __forceinline__ void hold(int32_t t, uint32_t* flags) {
+    const int lane = threadIdx.x & 63;
+    held = t;
+    const int64_t tok = begin + (static_cast<int64_t>(t) + static_cast<int64_t>(lane) * step) * 32;
+    page0 = tok < end ? table[tok >> shift] : -1;
+    page1 = tok + 16 < end ? table[(tok + 16) >> shift] : -1;
+    if ((tok < end && (page0 < 0 || page0 >= n_pages)) || (tok + 16 < end && (page1 < 0 || page1 >= n_pages))) {
+      raise(flags, LB_KV_BAD_PAGE);
+      if (page0 >= n_pages) page0 = -1;
+      if (page1 >= n_pages) page1 = -1;
     }
   }
-  const uint8_t* ks = block + P * D + (slot + n) * (D / 32) + (j * D) / 128;
-  H.ks = D == 256 ? *reinterpret_cast<const uint16_t*>(ks) : *ks;
-  H.vs = *reinterpret_cast<const uint32_t*>(block + P * D + P * D / 32 + (((slot >> 2) + j) * (D / 32) + (n * D) / 512) * 4);
-}
 
-__device__ __forceinline__ bool any_poison(uint32_t w) {
-  return ((w & 0xFFu) == 0xFFu) || ((w & 0xFF00u) == 0xFF00u) || ((w & 0xFF0000u) == 0xFF0000u) || (w >> 24) == 0xFFu;
-}
-
-// A workgroup takes 16 query rows of one sequence and KV head and one part of
-// their key range; its four wavefronts take every fourth tile and join at the end.
-template <int D, typename T>
-__global__ __launch_bounds__(256) void k_attend(AttendArgs A) {
-  constexpr int NP = Pieces<T>::n, KC = D / 32, VC = D / 16;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, j = lane >> 4;
-  const int32_t split = blockIdx.x % A.splits;
-  int64_t rest = blockIdx.x / A.splits;
-  const int32_t h = static_cast<int32_t>(rest % A.kv.kv_heads);
-  rest /= A.kv.kv_heads;
-  const int32_t tile = static_cast<int32_t>(rest % A.tiles), s = static_cast<int32_t>(rest / A.tiles);
-  const Seq q = sequence(A.kv, s);
-  if (q.bad && tile == 0 && h == 0 && split == 0 && threadIdx.x == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
-  const int32_t G = A.kv.q_heads / A.kv.kv_heads;
-  const int32_t R = q.count * G, r0 = tile * 16;
-  if (r0 >= R) return;
-  const bool live = r0 + n < R;
-  const int32_t i_tok = (r0 + n) / G, g = (r0 + n) % G;
-  const int32_t pos = live ? q.pos0 + i_tok : -1;
-  const int64_t row = q.row0 + static_cast<int64_t>(i_tok);
-  const int32_t hq = h * G + g;
-
-  // keys that some row of the tile sees, and this part of them
-  const int32_t p_first = q.pos0 + r0 / G;
-  const int32_t p_last = q.pos0 + (min(R, r0 + 16) - 1) / G;
-  const int32_t end = min(q.len, p_last + 1);
-  const int32_t begin = A.window > 0 ? max(0, p_first - A.window + 1) & ~31 : 0;
-  const int32_t tiles = end > begin ? (end - begin + 31) >> 5 : 0;
-  const int32_t per = (tiles + A.splits - 1) / A.splits;
-  const int32_t t_lo = split * per, t_hi = min(tiles, t_lo + per);
-
-  bf16x8 qf[KC][NP];
-#pragma unroll
-  for (int c = 0; c < KC; ++c) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (live) load8(static_cast<const T*>(A.q) + row * A.q_stride + hq * D + j * (D / 4) + c * 8, x);
-    split8<NP>(x, qf[c]);
-  }
-
-  f32x4 o[VC];
-#pragma unroll
-  for (int c = 0; c < VC; ++c) o[c] = f32x4{0, 0, 0, 0};
-  float m = -__builtin_inff(), l = 0.0f;
-
-  for (int32_t t = t_lo + wave; t < t_hi; t += 4) {
-    const int32_t tb = begin + t * 32;
-    Half<D> H[2];
-    load_half<D>(A.kv, s, h, tb, end, n, j, H[0]);
-    load_half<D>(A.kv, s, h, tb + 16, end, n, j, H[1]);
-    float sc[8];
-    bool seen[8];
+  // loads tile t; bit u of the result: half u exists
+  __device__ __forceinline__ int load(int32_t t, Tile<D>& X, uint32_t* flags) {
+    int32_t i = (t - held) / step;
+    if (i >= 64 || i < 0) {
+      hold(t, flags);
+      i = 0;
+    }
+    int ok = 0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      f32x4 acc{0, 0, 0, 0};
+      const int32_t page = __builtin_amdgcn_readlane(u ? page1 : page0, i);
+      if (page < 0) continue;  // what the registers hold stays unseen
+      ok |= 1 << u;
+      const int32_t slot = (begin + t * 32 + 16 * u) & ((1 << shift) - 1);
+      const uint8_t* at = base + page * page_bytes + slot * (D / 2);
+      const uint8_t* scales = base + page * page_bytes + slot * (D / 32);
+      if constexpr (D == 64) {
+        const u32x2 a = *reinterpret_cast<const u32x2*>(at + k_at), b = *reinterpret_cast<const u32x2*>(at + v_at);
+        X.k[u][0] = a.x, X.k[u][1] = a.y, X.v[u][0] = b.x, X.v[u][1] = b.y;
+      } else {
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        // channels j D/4 + 8 c .. + 7 lie in block (8 c) / 32 of the quarter (D = 256 has two there)
-        const uint32_t byte = D == 256 ? (H[u].ks >> (c < KC / 2 ? 0 : 8)) & 255u : H[u].ks;
-        const bf16x8 kf = bf16_of(H[u].k[c], scale_of(byte));
+        for (int c = 0; c < D / 128; ++c) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(at + k_at + 16 * c), b = *reinterpret_cast<const u32x4*>(at + v_at + 16 * c);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) acc = mfma(kf, qf[c][p], acc);
+          for (int x = 0; x < 4; ++x) X.k[u][4 * c + x] = a[x], X.v[u][4 * c + x] = b[x];
+        }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int32_t tok = tb + 16 * u + 4 * j + i;
-        const bool vis = H[u].ok && tok < end && tok <= pos && (A.window <= 0 || tok > pos - A.window);
-        seen[4 * u + i] = vis;
-        sc[4 * u + i] = vis ? acc[i] * A.scale2 : -__builtin_inff();
-      }
+      X.ks[u] = D == 256 ? *reinterpret_cast<const uint16_t*>(scales + ks_at) : scales[ks_at];
+      X.vs[u] = *reinterpret_cast<const uint32_t*>(scales + vs_at);
     }
-    float mx = m;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, sc[i]);
-    mx = row_max(mx);
-    const float base = mx == -__builtin_inff() ? 0.0f : mx;  // nothing seen yet: every exponent is -infinity
-    const float fade = __builtin_amdgcn_exp2f(m - base);
-    m = mx;
-    l *= fade;
-    float p[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(sc[i] - base);
-      l += p[i];
-    }
-#pragma unroll
-    for (int c = 0; c < VC; ++c) o[c] *= fade;
-    bf16x8 pf[NP];
-    split8<NP>(p, pf);
+    return ok;
+  }
+};
 
-    // the values' scales; tokens that no row sees count as 0, whatever the cache holds there
+// The state of QT tiles of 16 query rows in one wavefront.
+template <int D, int NP, int QT>
+struct Rows {
+  static constexpr int KC = D / 32, VC = D / 16;
+  bf16x8 q[QT][KC][NP];
+  f32x4 o[QT][VC];
+  float m[QT], l[QT];  // reference and the lane's share of the sum of exp2(score - reference)
+  int32_t pos[QT];     // the lane's row's position, -1: no row
+  float scale2;        // log2(e) |scale|, its sign is in q
+  int32_t window, end, p_min, p_max;  // p_min, p_max: over the rows there are
+
+  // How far a score may pass the reference before the reference moves: sums of
+  // exp2 keep their precision, and most tiles need no exchange between lanes.
+  static constexpr float kSlack = 8.0f;
+
+  // One tile of keys and values.  edge: some row does not see some of its tokens.
+  __device__ __forceinline__ void take(const Tile<D>& X, int32_t tb, int ok, bool edge, int j) {
+    f32x4 acc[QT][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 kf[KC];
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+        // channels j D/4 + 8 c .. + 7 lie in block (8 c) / 32 of the quarter (D = 256 has two there)
+        kf[c] = bf16_of(X.k[u][c], scale_of(D == 256 ? (X.ks[u] >> (c < KC / 2 ? 0 : 8)) & 255u : X.ks[u]));
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        acc[t][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) acc[t][u] = mfma(kf[c], q[t][c][p], acc[t][u]);
+      }
+    }
+    if (edge) {
+      asm volatile("");  // a branch: most tiles are whole
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!seen(t, tb + 16 * u + 4 * j + i, ok >> u & 1)) acc[t][u][i] = -__builtin_inff();
+    }
+    bf16x8 pf[QT][NP];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float top = larger(larger(larger(acc[t][0][0], acc[t][0][1]), larger(acc[t][0][2], acc[t][0][3])),
+                         larger(larger(acc[t][1][0], acc[t][1][1]), larger(acc[t][1][2], acc[t][1][3])));
+      top *= scale2;
+      if (__any(top > m[t] + kSlack)) {
+        const float mx = fmaxf(m[t], row_max(top));
+        const float fade = mx == m[t] ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mx);
+        m[t] = mx;
+        l[t] *= fade;
+#pragma unroll
+        for (int c = 0; c < VC; ++c) o[t][c] *= fade;
+      }
+      const float base = m[t] == -__builtin_inff() ? 0.0f : m[t];  // nothing seen yet: every exponent is -infinity
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(acc[t][i >> 2][i & 3], scale2, -base));
+        l[t] += p[i];
+      }
+      split8<NP>(p, pf[t]);
+    }
+
+    // the values' scales; tokens that no row sees count as 0, whatever the cache
+    // holds there, and blocks of NaN too at first
+    uint32_t bytes[2] = {X.vs[0], X.vs[1]};
+    if (edge) {
+      asm volatile("");
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t left = ok >> u & 1 ? end - (tb + 16 * u + 4 * j) : 0;
+        bytes[u] = left >= 4 ? bytes[u] : left <= 0 ? 0u : bytes[u] & ((1u << (8 * left)) - 1u);
+      }
+    }
     float vs[2][4];
-    bool poison = false;
+    const uint32_t nan[2] = {bytes_255(bytes[0]), bytes_255(bytes[1])};
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t byte = H[u].vs >> (8 * i) & 255u;
-        const bool in = tb + 16 * u + 4 * j + i < end;
-        poison |= in && byte == kPoison;
-        vs[u][i] = scale_of(in && byte != kPoison ? byte : 0u);
-      }
+      for (int i = 0; i < 4; ++i) vs[u][i] = scale_of((bytes[u] & ~nan[u]) >> (8 * i) & 255u);
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {
       uint32_t y[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(H[u].v[w], vs[u][0], 0));
-        y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(H[u].v[w], vs[u][1], 1));
-        y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(H[u].v[w], vs[u][2], 2));
-        y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(H[u].v[w], vs[u][3], 3));
+        y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][0], 0));
+        y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][1], 1));
+        y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][2], 2));
+        y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][3], 3));
       }
 #pragma unroll
       for (int par = 0; par < 2; ++par) {
@@ -599,28 +630,153 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs A) {
                       __builtin_amdgcn_perm(y[1][1], y[1][0], sel), __builtin_amdgcn_perm(y[1][3], y[1][2], sel)};
         const bf16x8 vf = __builtin_bit_cast(bf16x8, f);
 #pragma unroll
-        for (int k = 0; k < NP; ++k) o[2 * w + par] = mfma(vf, pf[k], o[2 * w + par]);
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) o[t][2 * w + par] = mfma(vf, pf[t][p], o[t][2 * w + par]);
       }
     }
-    if (__any(poison)) {
-      // a block of NaN reaches the rows that see its token, and no other: 0 * NaN
-      // in the products above would reach all of them
-      bf16x8 bad, vis;
+    if (__any((nan[0] | nan[1]) != 0)) spread_nan(nan, tb, ok, j);
+  }
+
+  __device__ __forceinline__ bool seen(int t, int32_t tok, bool ok) const {
+    return ok && tok < end && tok <= pos[t] && (window <= 0 || tok > pos[t] - window);
+  }
+
+  // A block of NaN reaches the rows that see its token, and no other: 0 * NaN in
+  // the products would reach all of them.  So a product of what is NaN with what
+  // is seen says which results it reaches.
+  __device__ __forceinline__ void spread_nan(const uint32_t (&nan)[2], int32_t tb, int ok, int j) {
+    asm volatile("");  // a branch: there is no such block as a rule
+    bf16x8 bad;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool b = (H[i >> 2].vs >> (8 * (i & 3)) & 255u) == kPoison && tb + 16 * (i >> 2) + 4 * j + (i & 3) < end;
-        bad[i] = static_cast<__bf16>(b ? 1.0f : 0.0f);
-        vis[i] = static_cast<__bf16>(seen[i] ? 1.0f : 0.0f);
-      }
+    for (int i = 0; i < 8; ++i) bad[i] = static_cast<__bf16>(nan[i >> 2] >> (8 * (i & 3)) & 1u ? 1.0f : 0.0f);
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      bf16x8 vis;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        vis[i] = static_cast<__bf16>(seen(t, tb + 16 * (i >> 2) + 4 * j + (i & 3), ok >> (i >> 2) & 1) ? 1.0f : 0.0f);
       const f32x4 hit = mfma(bad, vis, f32x4{0, 0, 0, 0});
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (hit[i] > 0.0f)
 #pragma unroll
-          for (int c = 0; c < VC; ++c) o[c][i] = __builtin_nanf("");
+          for (int c = 0; c < VC; ++c) o[t][c][i] = __builtin_nanf("");
     }
   }
-  l = row_sum(l);
+
+  // All tiles of a key range, the next tile's loads in flight during each.
+  __device__ __forceinline__ void sweep(Keys<D>& K, int32_t t, int32_t t_hi, int j, uint32_t* flags) {
+    Tile<D> X{}, Y{};
+    int ok = t < t_hi ? K.load(t, X, flags) : 0;
+    for (; t < t_hi; t += K.step) {
+      const int next = t + K.step < t_hi ? K.load(t + K.step, Y, flags) : 0;
+      const int32_t tb = K.begin + t * 32;
+      // every row sees the whole tile
+      const bool inner = ok == 3 && tb + 31 <= p_min && tb + 32 <= end && (window <= 0 || tb > p_max - window);
+      take(X, tb, ok, !inner, j);
+      X = Y;
+      ok = next;
+    }
+  }
+};
+
+// Wavefronts a SIMD that the registers are bounded for: as many as go without
+// spilling (o and q take 4 D/16 + 4 D/32 NP registers a row tile).
+constexpr int waves(int D, int pieces, int QT) { return D * QT * (1 + pieces) <= 256 ? 3 : D * QT * (1 + pieces) <= 768 ? 2 : 1; }
+
+// query row tiles of 16 a wavefront holds where there are many rows
+__host__ __device__ constexpr int row_tiles(int D, int pieces) { return D * (1 + pieces) <= 384 ? 2 : 1; }
+
+// What a workgroup has to do: rows r0 .. of a sequence and KV head.
+struct Job {
+  Seq q;
+  int32_t s, h, tile, split, G, R;
+};
+__device__ __forceinline__ Job job_of(const AttendArgs& A) {
+  Job w;
+  w.split = blockIdx.x % A.splits;
+  uint32_t rest = blockIdx.x / A.splits;
+  w.h = static_cast<int32_t>(rest % A.kv.kv_heads);
+  rest /= A.kv.kv_heads;
+  w.s = static_cast<int32_t>(rest / A.tiles);
+  w.tile = A.tiles - 1 - static_cast<int32_t>(rest % A.tiles);  // the last rows see most keys: they go first
+  w.q = sequence(A.kv, w.s);
+  if (w.q.bad && w.tile == 0 && w.h == 0 && w.split == 0 && threadIdx.x == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+  w.G = A.kv.q_heads / A.kv.kv_heads;
+  w.R = w.q.count * w.G;
+  return w;
+}
+
+// Rows r0 .. r0 + 16 QT - 1 of the job into a wavefront's state; false: there are none.
+template <int D, typename T, int QT>
+__device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32_t r0, Rows<D, Pieces<T>::n, QT>& S, int n, int j) {
+  if (r0 >= w.R) return false;
+  S.scale2 = fabsf(A.scale2);
+  float sign = A.scale2 < 0.0f ? -1.0f : 1.0f;
+  if (A.scale2 == 0.0f) sign = 0.0f, S.scale2 = 1.0f;
+  S.window = A.window;
+  S.p_min = w.q.pos0 + r0 / w.G;
+  S.p_max = w.q.pos0 + (min(w.R, r0 + 16 * QT) - 1) / w.G;
+  S.end = min(w.q.len, S.p_max + 1);
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int32_t r = r0 + 16 * t + n;
+    const bool live = r < w.R;
+    const int32_t i = r / w.G, g = r % w.G;
+    S.pos[t] = live ? w.q.pos0 + i : -1;
+    S.m[t] = -__builtin_inff();
+    S.l[t] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) S.o[t][c] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (live) load8(static_cast<const T*>(A.q) + (w.q.row0 + static_cast<int64_t>(i)) * A.q_stride + (w.h * w.G + g) * D + j * (D / 4) + c * 8, x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] *= sign;
+      split8<Pieces<T>::n>(x, S.q[t][c]);
+    }
+  }
+  return true;
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_channels(T* dst, const float (&x)[N]) {
+  if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int c = 0; c < N; c += 8) {
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = x[c + i];
+      store8(dst + c, y);
+    }
+  } else if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(dst) = f32x4{x[0], x[1], x[2], x[3]};
+  } else {
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<T4*>(dst) = T4{static_cast<T>(x[0]), static_cast<T>(x[1]), static_cast<T>(x[2]), static_cast<T>(x[3])};
+  }
+}
+
+__device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }  // l may be NaN
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -__builtin_inff() : (m + log2f(l)) * 0.6931471805599453f; }
+
+// Few query rows: a workgroup takes 16 rows and one part of their key range; its
+// four wavefronts take every fourth tile and join at the end.
+template <int D, typename T>
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
+  constexpr int VC = D / 16;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
+  const Job w = job_of(A);
+  Rows<D, Pieces<T>::n, 1> S;
+  if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
+  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
+  const int32_t tiles = S.end > begin ? (S.end - begin + 31) >> 5 : 0;
+  const int32_t per = (tiles + A.splits - 1) / A.splits;
+  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 4, n, j);
+  S.sweep(K, w.split * per + wave, min(tiles, (w.split + 1) * per), j, A.kv.flags);
+  const float l = row_sum(S.l[0]);
 
   // join the four wavefronts
   __shared__ float part[4][VC * 4][64];
@@ -628,71 +784,128 @@ __global__ __launch_bounds__(256) void k_attend(AttendArgs A) {
 #pragma unroll
   for (int c = 0; c < VC; ++c)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) part[wave][4 * c + i][lane] = o[c][i];
-  if (j == 0) pm[wave][n] = m, pl[wave][n] = l;
+    for (int i = 0; i < 4; ++i) part[wave][4 * c + i][lane] = S.o[0][c][i];
+  if (j == 0) pm[wave][n] = S.m[0], pl[wave][n] = l;
   __syncthreads();
   const float M = fmaxf(fmaxf(pm[0][n], pm[1][n]), fmaxf(pm[2][n], pm[3][n]));
   const float base = M == -__builtin_inff() ? 0.0f : M;
   float wgt[4], L = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    wgt[w] = __builtin_amdgcn_exp2f(pm[w][n] - base);
-    L += wgt[w] * pl[w][n];
+  for (int k = 0; k < 4; ++k) {
+    wgt[k] = __builtin_amdgcn_exp2f(pm[k][n] - base);
+    L += wgt[k] * pl[k][n];
   }
-  if (!live) return;
-  // wave w writes the rows 4 j + w of the results: D/16 adjacent channels a lane
+  const int32_t r = w.tile * 16 + n;
+  if (r >= w.R) return;
+  const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
+  const int32_t hq = w.h * w.G + r % w.G;
+  // wavefront i writes the rows 4 j + i of the results: D/16 adjacent channels a lane
   const int i = wave;
   float x[VC];
 #pragma unroll
   for (int c = 0; c < VC; ++c) {
     x[c] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) x[c] += wgt[w] * part[w][4 * c + i][lane];
+    for (int k = 0; k < 4; ++k) x[c] += wgt[k] * part[k][4 * c + i][lane];
   }
   const int32_t ch = (4 * j + i) * (D / 16);
+  const int64_t at = row * A.kv.q_heads + hq;
   if (A.splits > 1) {
-    const int64_t slot = (row * A.kv.q_heads + hq) * A.splits + split;
-    float* dst = A.part + slot * (D + 2);
-    if (i == 0 && j == 0) dst[D] = M, dst[D + 1] = L;
-#pragma unroll
-    for (int c = 0; c < VC; ++c) dst[ch + c] = x[c];
+    store_channels<VC>(A.part + (at * A.splits + w.split) * D + ch, x);
+    if (i == 0 && j == 0) {
+      float* sums = A.part + static_cast<int64_t>(A.kv.n_rows) * A.kv.q_heads * A.splits * D + (at * A.splits + w.split) * 2;
+      sums[0] = M, sums[1] = L;
+    }
     return;
   }
-  const float inv = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;  // L may be NaN
-  T* dst = static_cast<T*>(A.out) + row * A.out_stride + hq * D + ch;
+  const float inv = inverse(L);
 #pragma unroll
-  for (int c = 0; c < VC; ++c) dst[c] = static_cast<T>(x[c] * inv);
-  if (A.lse && i == 0 && j == 0)
-    A.lse[row * A.kv.q_heads + hq] = L == 0.0f ? -__builtin_inff() : (base + log2f(L)) * 0.6931471805599453f;
+  for (int c = 0; c < VC; ++c) x[c] *= inv;
+  store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + ch, x);
+  if (A.lse && i == 0 && j == 0) A.lse[at] = lse_of(base, L);
 }
 
-// Joins the parts of a row's key range: a wavefront per (new token, query head).
-template <int D, typename T>
-__global__ __launch_bounds__(64) void k_attend_join(AttendArgs A) {
-  const int32_t hq = blockIdx.y;
-  const int64_t row = blockIdx.x;
-  if (row < A.kv.starts[0] || row >= A.kv.starts[A.kv.n_seqs]) return;  // padding
-  const int lane = threadIdx.x;
-  const float* src = A.part + (row * A.kv.q_heads + hq) * A.splits * (D + 2);
-  float M = -__builtin_inff();
-  for (int32_t k = 0; k < A.splits; ++k) M = fmaxf(M, src[k * (D + 2) + D]);
-  const float base = M == -__builtin_inff() ? 0.0f : M;
-  float L = 0.0f, x[D / 64];
+// Many query rows: each of the four wavefronts takes 16 QT rows of its own and
+// walks all keys that these see.
+template <int D, typename T, int QT>
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows(AttendArgs A) {
+  constexpr int VC = D / 16;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
+  const Job w = job_of(A);
+  Rows<D, Pieces<T>::n, QT> S;
+  const int32_t r0 = (w.tile * 4 + wave) * 16 * QT;
+  if (!rows_of<D, T, QT>(A, w, r0, S, n, j)) return;
+  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
+  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
+  S.sweep(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c) x[c] = 0.0f;
-  for (int32_t k = 0; k < A.splits; ++k) {
-    const float* p = src + k * (D + 2);
-    const float w = __builtin_amdgcn_exp2f(p[D] - base);
-    L += w * p[D + 1];
+  for (int t = 0; t < QT; ++t) {
+    const float L = row_sum(S.l[t]), inv = inverse(L);
+    const int32_t r = r0 + 16 * t + n;
+    if (r >= w.R) continue;
+    const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
+    const int32_t hq = w.h * w.G + r % w.G;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) x[c] += w * p[c * 64 + lane];
+    for (int i = 0; i < 4; ++i) {
+      float x[VC];
+#pragma unroll
+      for (int c = 0; c < VC; ++c) x[c] = S.o[t][c][i] * inv;
+      store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + (4 * j + i) * (D / 16), x);
+    }
+    if (A.lse && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(S.m[t], L);
   }
-  const float inv = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
-  T* dst = static_cast<T*>(A.out) + row * A.out_stride + hq * D;
+}
+
+// Joins the parts of a row's key range: a workgroup per (new token, query head),
+// whose wavefronts take every fourth part.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
+  constexpr int N = D / 64;
+  const int64_t row = blockIdx.x / A.kv.q_heads;
+  if (row < A.kv.starts[0] || row >= A.kv.starts[A.kv.n_seqs]) return;  // padding
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  const int32_t hq = blockIdx.x % A.kv.q_heads;
+  const int64_t at = blockIdx.x;
+  const float* parts = A.part + at * A.splits * D;
+  const float* sums = A.part + static_cast<int64_t>(A.kv.n_rows) * A.kv.q_heads * A.splits * D + at * A.splits * 2;
+  // lane i: the sums of parts i and 64 + i
+  float m[2], l[2], M = -__builtin_inff();
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c) dst[c * 64 + lane] = static_cast<T>(x[c] * inv);
-  if (A.lse && lane == 0)
-    A.lse[row * A.kv.q_heads + hq] = L == 0.0f ? -__builtin_inff() : (base + log2f(L)) * 0.6931471805599453f;
+  for (int k = 0; k < 2; ++k) {
+    const bool have = lane + 64 * k < A.splits;
+    m[k] = have ? sums[2 * (lane + 64 * k)] : -__builtin_inff();
+    l[k] = have ? sums[2 * (lane + 64 * k) + 1] : 0.0f;
+    M = fmaxf(M, m[k]);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
+  const float base = M == -__builtin_inff() ? 0.0f : M;
+  float L = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    m[k] = __builtin_amdgcn_exp2f(m[k] - base);
+    L += m[k] * l[k];
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
+  float x[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c) x[c] = 0.0f;
+#pragma unroll 4
+  for (int32_t k = wave; k < A.splits; k += 4) {
+    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k < 64 ? m[0] : m[1]), k & 63));
+#pragma unroll
+    for (int c = 0; c < N; ++c) x[c] += f * parts[k * D + c * 64 + lane];
+  }
+  __shared__ float joined[4][D];
+#pragma unroll
+  for (int c = 0; c < N; ++c) joined[wave][c * 64 + lane] = x[c];
+  __syncthreads();
+  const float inv = inverse(L);
+  T* dst = static_cast<T*>(A.out) + row * A.out_stride + hq * D;
+  for (int c = threadIdx.x; c < D; c += 256)
+    dst[c] = static_cast<T>((joined[0][c] + joined[1][c] + joined[2][c] + joined[3][c]) * inv);
+  if (A.lse && threadIdx.x == 0) A.lse[at] = lse_of(base, L);
 }
 
 int64_t units(const KvArgs& A) { return A.max_new == 1 ? A.n_seqs : A.n_rows / 4 + 2ll * A.n_seqs; }
@@ -714,10 +927,14 @@ hipError_t read(const ReadArgs& A, hipStream_t st) {
 template <int D, typename T>
 hipError_t attend(const AttendArgs& A, hipStream_t st) {
   const int64_t blocks = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads * A.splits;
+  if (A.by_rows) {
+    k_attend_rows<D, T, row_tiles(D, Pieces<T>::n)><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
+    return hipGetLastError();
+  }
   k_attend<D, T><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.splits == 1) return e;
-  k_attend_join<D, T><<<dim3(static_cast<unsigned>(A.kv.n_rows), static_cast<unsigned>(A.kv.q_heads)), 64, 0, st>>>(A);
+  k_attend_join<D, T><<<dim3(static_cast<unsigned>(A.kv.n_rows * A.kv.q_heads)), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
@@ -736,18 +953,24 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(read); }
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(attend); }
 
-// Tiles of 16 query rows a sequence may have, and the parts of its key range:
-// so many that about four workgroups a CU exist, each with 8 tiles of keys at least.
-AttendPlan attend_plan(const KvArgs& kv, int head_dim) {
+// How a call is cut up.  Few query rows a sequence and KV head: tiles of 16 rows,
+// and parts of the key range so that about eight workgroups a CU exist, each with
+// 16 tiles of keys at least.  Many: a workgroup takes its wavefronts' rows.
+AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   AttendPlan p;
   const int64_t rows = static_cast<int64_t>(kv.max_new) * (kv.q_heads / kv.kv_heads);
-  p.tiles = static_cast<int32_t>((rows + 15) / 16);
+  const int64_t per = 4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3);
+  p.by_rows = rows > 64;
+  p.tiles = static_cast<int32_t>(p.by_rows ? (rows + per - 1) / per : (rows + 15) / 16);
+  p.splits = 1;
+  p.part_floats = 0;
+  if (p.by_rows) return p;
   const int64_t blocks = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;
   const int64_t tokens = static_cast<int64_t>(kv.max_pages) << kv.page_shift;
-  int64_t s = blocks > 0 ? (1024 + blocks - 1) / blocks : 1;
-  s = s < tokens / 256 ? s : tokens / 256;
+  int64_t s = blocks > 0 ? (2048 + blocks - 1) / blocks : 1;
+  s = s < tokens / 512 ? s : tokens / 512;
   p.splits = static_cast<int32_t>(s < 1 ? 1 : s > 128 ? 128 : s);
-  p.part_floats = p.splits > 1 ? static_cast<int64_t>(kv.n_rows) * kv.q_heads * p.splits * (head_dim + 2) : 0;
+  if (p.splits > 1) p.part_floats = static_cast<int64_t>(kv.n_rows) * kv.q_heads * p.splits * (head_dim + 2);
   return p;
 }
 

@@ -2,8 +2,15 @@
 //
 // A row is read once for its maximum and sum (kept together, the sum rescaled
 // when the maximum grows) and once more where its log-probabilities are wanted.
-// The few classes that a history or a bias list names are found through a table
-// in LDS behind a filter of one bit per class number modulo 65536.
+//
+// Long rows: a workgroup takes a part of a row, 16 B a lane at a time.  The
+// classes that a history or a bias list names are few: they are left out of that
+// sweep, as the masked ones are, by one bit a class in LDS, and handled on their
+// own from a hash table of at most LB_MAX_RULE_IDS entries, so the sweep has no
+// branch for them.
+//
+// Short rows (up to 512 classes): 16 or 64 lanes hold a row in registers and
+// read it once.
 #include <hip/hip_runtime.h>
 
 #include "lb_scorer.h"
@@ -12,76 +19,9 @@ namespace lb {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kFilterWords = 65536 / 32;
-
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__bf16 x) { return static_cast<float>(x); }
 __device__ __forceinline__ float as_float(_Float16 x) { return static_cast<float>(x); }
-
-struct Slot {
-  int32_t id;      // -1: empty
-  int32_t count;   // occurrences in the history
-  int32_t bias;    // place in the bias list + 1, 0: none
-};
-
-// The classes that the row's history and bias list name.  `slots` (a power of
-// two, at least twice as many as there may be names; 0: no names at all)
-struct Named {
-  uint32_t* filter;
-  Slot* table;
-  int32_t slots;
-  const float* bias;
-};
-
-__device__ __forceinline__ void put(const Named& N, int32_t id, int32_t count, int32_t bias) {
-  atomicOr(&N.filter[(id & 65535) >> 5], 1u << (id & 31));
-  uint32_t at = (static_cast<uint32_t>(id) * 2654435761u) & (N.slots - 1);
-  for (;;) {
-    const int32_t was = atomicCAS(&N.table[at].id, -1, id);
-    if (was == -1 || was == id) break;
-    at = (at + 1) & (N.slots - 1);
-  }
-  if (count) atomicAdd(&N.table[at].count, count);
-  if (bias) atomicMax(&N.table[at].bias, bias);
-}
-
-__device__ __forceinline__ Named names(const LogitArgs& A, int64_t row, int32_t slots, uint32_t* shared) {
-  Named N{shared, reinterpret_cast<Slot*>(shared + kFilterWords), slots, nullptr};
-  if (!slots) return N;
-  for (int i = threadIdx.x; i < kFilterWords; i += blockDim.x) N.filter[i] = 0;
-  for (int i = threadIdx.x; i < slots; i += blockDim.x) N.table[i] = Slot{-1, 0, 0};
-  __syncthreads();
-  for (int i = threadIdx.x; i < A.r.history_width; i += blockDim.x) {
-    const int32_t id = A.r.history[row * A.r.history_width + i];
-    if (id >= 0 && id < A.classes) put(N, id, 1, 0);
-  }
-  const int64_t list = A.r.bias_per_row ? row * A.r.bias_width : 0;
-  N.bias = A.r.bias_values + list;
-  for (int i = threadIdx.x; i < A.r.bias_width; i += blockDim.x) {
-    const int32_t id = A.r.bias_ids[list + i];
-    if (id >= 0 && id < A.classes) put(N, id, 0, i + 1);
-  }
-  __syncthreads();
-  return N;
-}
-
-__device__ __forceinline__ float adjusted(const LogitArgs& A, const Named& N, const uint32_t* mask, int32_t w, float x) {
-  if (N.slots && (N.filter[(w & 65535) >> 5] >> (w & 31) & 1u)) {
-    uint32_t at = (static_cast<uint32_t>(w) * 2654435761u) & (N.slots - 1);
-    while (N.table[at].id != -1 && N.table[at].id != w) at = (at + 1) & (N.slots - 1);
-    const Slot s = N.table[at];
-    if (s.id == w) {
-      if (s.count) {
-        x = x > 0.0f ? x / A.r.repetition : x * A.r.repetition;
-        x = x - A.r.presence - A.r.frequency * static_cast<float>(s.count);
-      }
-      if (s.bias) x += N.bias[s.bias - 1];
-    }
-  }
-  if (A.r.temperature != 1.0f) x /= A.r.temperature;
-  if (mask && !(mask[w >> 5] >> (w & 31) & 1u)) x = -__builtin_inff();
-  return x;
-}
 
 __device__ __forceinline__ const uint32_t* mask_of(const LogitArgs& A, int64_t row) {
   if (!A.r.mask) return nullptr;
@@ -89,21 +29,67 @@ __device__ __forceinline__ const uint32_t* mask_of(const LogitArgs& A, int64_t r
   return k >= 0 && k < A.r.mask_rows ? A.r.mask + k * ((A.classes + 31) / 32) : nullptr;
 }
 
+// The rules for one class, in the order that the header gives.  The divisions
+// are products with the rounded reciprocals: one rounding of 2^-24 more.
+struct Rules {
+  float inv_temperature, repetition, inv_repetition, presence, frequency;
+  __device__ __forceinline__ explicit Rules(const lb_logit_rules& r)
+      : inv_temperature(1.0f / r.temperature), repetition(r.repetition), inv_repetition(1.0f / r.repetition),
+        presence(r.presence), frequency(r.frequency) {}
+  __device__ __forceinline__ float operator()(float x, int32_t count, float bias) const {
+    if (count) x = x * (x > 0.0f ? inv_repetition : repetition) - presence - frequency * static_cast<float>(count);
+    return (x + bias) * inv_temperature;
+  }
+};
+
 // (m, l): a maximum and the sum of exp2(log2(e) (z - m)); nothing yet: (-inf, 0)
 struct Sum {
   float m, l;
 };
 // what exponents are taken relative to: an infinite maximum would make inf - inf of them
 __device__ __forceinline__ float safe(float m) { return __builtin_isinf(m) ? 0.0f : m; }
-__device__ __forceinline__ void add(Sum& a, float z) {
-  const float m = fmaxf(a.m, z), base = safe(m);
-  a.l = a.l * __builtin_amdgcn_exp2f((a.m - base) * kLog2e) + __builtin_amdgcn_exp2f((z - base) * kLog2e);
-  a.m = m;
-}
+__device__ __forceinline__ float exp_of(float z, float base) { return __builtin_amdgcn_exp2f((z - base) * kLog2e); }
 __device__ __forceinline__ void join(Sum& a, float m2, float l2) {
   const float m = fmaxf(a.m, m2), base = safe(m);
-  a.l = a.l * __builtin_amdgcn_exp2f((a.m - base) * kLog2e) + l2 * __builtin_amdgcn_exp2f((m2 - base) * kLog2e);
+  a.l = a.l * exp_of(a.m, base) + l2 * exp_of(m2, base);
   a.m = m;
+}
+// n values at once: one rescaling of the sum
+template <int n>
+__device__ __forceinline__ void add(Sum& a, const float (&z)[n]) {
+  float m = a.m;
+#pragma unroll
+  for (int i = 0; i < n; ++i) m = fmaxf(m, z[i]);
+  const float base = safe(m);
+  float l = a.l * exp_of(a.m, base);
+#pragma unroll
+  for (int i = 0; i < n; ++i) l += exp_of(z[i], base);
+  a.l = l;
+  a.m = m;
+}
+// sum or maximum over the 16 or 64 lanes of a row, by moves within a row of 16
+// lanes (pairs, quads, and mirrored halves, where each half has one value already)
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct Plus {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+template <int ctrl>
+__device__ __forceinline__ float moved(float x) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl, 0xF, 0xF, true));
+}
+template <int L, typename F>
+__device__ __forceinline__ float over_lanes(float x, F f) {
+  x = f(x, moved<0xB1>(x));   // lanes 1 0 3 2
+  x = f(x, moved<0x4E>(x));   // lanes 2 3 0 1
+  x = f(x, moved<0x141>(x));  // row_half_mirror
+  x = f(x, moved<0x140>(x));  // row_mirror
+  if constexpr (L == 64) {
+    x = f(x, __shfl_xor(x, 16));
+    x = f(x, __shfl_xor(x, 32));
+  }
+  return x;
 }
 __device__ __forceinline__ Sum block_sum(Sum s) {
   __shared__ float sm[4], sl[4];
@@ -134,92 +120,343 @@ __device__ __forceinline__ void finish(const LogitArgs& A, int64_t row, Lse lse,
   A.score[row] = t < 0 ? 0.0f : t >= A.classes ? __builtin_nanf("") : log_prob(zt, lse);
 }
 
-// One part of a row: its sum, and the whole rest where the row has one part.
-// The parts' sums are kept at part[row][split] = (m, l) and the target's z after
-// them.
+// ------------------------------------------------------------------ long rows
+
+constexpr int kPartClasses = 131072;  // classes of one part at most: 16 KB of bits, eight workgroups a CU
+
+struct Slot {
+  int32_t id;     // -1: empty
+  int32_t count;  // occurrences in the history
+  int32_t bias;   // place in the bias list + 1, 0: none
+  float z;        // the class's logit after the rules
+};
+
+// A part of a row: the classes lo .. hi - 1, in chunks of eight that start at
+// 16-B aligned logits (the first and last may be cut short).  bit 8 c + i of
+// `open` is set where class i of chunk c is in the part, allowed by the mask and
+// not named.
+template <typename T>
+struct Part {
+  const T* src;     // logits of the row
+  int32_t lo, hi, first;  // class at bit 0
+  int32_t chunks;
+  uint8_t* open;
+  Slot* table;
+  int32_t slots;
+  bool sparse;  // some bit may be clear (other than outside the part)
+  float inv;
+
+  __device__ __forceinline__ void start(const LogitArgs& A, int64_t row, int32_t part, int32_t parts, int32_t n_slots, uint32_t* shared) {
+    const int32_t per = (A.classes + parts - 1) / parts;
+    lo = min(A.classes, part * per);
+    hi = min(A.classes, lo + per);
+    src = static_cast<const T*>(A.logits) + row * A.stride;
+    first = lo - static_cast<int32_t>((reinterpret_cast<uintptr_t>(src + lo) & 15) / sizeof(T));
+    chunks = (hi - first + 7) >> 3;
+    const Rules rules(A.r);
+    inv = rules.inv_temperature;
+    slots = n_slots;
+    const uint32_t* mask = mask_of(A, row);
+    sparse = mask || slots;
+    open = reinterpret_cast<uint8_t*>(shared);
+    const int32_t words = (chunks + 3) >> 2;
+    table = reinterpret_cast<Slot*>(shared + ((words + 3) & ~3));
+    if (!sparse) return;
+    for (int32_t i = threadIdx.x; i < words; i += 256) {
+      uint32_t w = 0xFFFFFFFFu;
+      if (mask) {
+        // classes first + 32 i .. + 31 of the mask (first may lie before class 0: those bits are not looked at)
+        const int32_t c = first + 32 * i, at = c >> 5, sh = c & 31, last = (A.classes - 1) >> 5;
+        const uint32_t a = at >= 0 ? mask[min(at, last)] : 0, b = at + 1 <= last ? mask[at + 1] : 0;
+        w = sh ? a >> sh | b << (32 - sh) : a;
+      }
+      shared[i] = w;
+    }
+    if (!slots) {
+      __syncthreads();
+      return;
+    }
+    for (int32_t i = threadIdx.x; i < slots; i += 256) table[i] = Slot{-1, 0, 0, 0.0f};
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < A.r.history_width; i += 256) put(A.r.history[row * A.r.history_width + i], 1, 0);
+    const int64_t list = A.r.bias_per_row ? row * A.r.bias_width : 0;
+    for (int32_t i = threadIdx.x; i < A.r.bias_width; i += 256) put(A.r.bias_ids[list + i], 0, i + 1);
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < slots; i += 256) {
+      Slot& s = table[i];
+      if (s.id < 0) continue;
+      const int32_t at = s.id - first;
+      if (shared[at >> 5] >> (at & 31) & 1u) {
+        atomicAnd(&shared[at >> 5], ~(1u << (at & 31)));
+        s.z = rules(as_float(src[s.id]), s.count, s.bias ? A.r.bias_values[list + s.bias - 1] : 0.0f);
+      } else {
+        s.z = -__builtin_inff();  // masked
+      }
+    }
+    __syncthreads();
+  }
+
+  __device__ __forceinline__ void put(int32_t id, int32_t count, int32_t bias) {
+    if (id < lo || id >= hi) return;
+    uint32_t at = (static_cast<uint32_t>(id) * 2654435761u) & (slots - 1);
+    for (;;) {
+      const int32_t was = atomicCAS(&table[at].id, -1, id);
+      if (was == -1 || was == id) break;
+      at = (at + 1) & (slots - 1);
+    }
+    if (count) atomicAdd(&table[at].count, count);
+    if (bias) atomicMax(&table[at].bias, bias);
+  }
+
+  // the logits of chunk c, -infinity where its bits are clear; false: the chunk is cut short
+  __device__ __forceinline__ bool load(int32_t c, float (&z)[8]) const {
+    const int32_t w = first + 8 * c;
+    const bool whole = w >= lo && w + 8 <= hi;
+    if (whole) {
+      load8(src + w, z);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = w + i >= lo && w + i < hi ? as_float(src[w + i]) : -__builtin_inff();
+    }
+    const uint32_t bits = sparse ? open[c] : 255u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = bits >> i & 1u ? z[i] * inv : -__builtin_inff();
+    return whole;
+  }
+
+  __device__ __forceinline__ Sum sum(int32_t target, float* zt) const {
+    Sum s{-__builtin_inff(), 0.0f};
+    for (int32_t c = threadIdx.x; c < chunks; c += 256) {
+      float z[8];
+      load(c, z);
+      add(s, z);
+      const uint32_t t = static_cast<uint32_t>(target - (first + 8 * c));
+      if (t < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (t == i && z[i] != -__builtin_inff()) *zt = z[i];
+      }
+    }
+    for (int32_t i = threadIdx.x; i < slots; i += 256) {
+      if (table[i].id < 0) continue;
+      const float z[1] = {table[i].z};
+      add(s, z);
+      if (table[i].id == target) *zt = z[0];
+    }
+    return s;
+  }
+
+  __device__ __forceinline__ void write(float* dst, Lse lse) const {
+    const bool even = ((reinterpret_cast<uintptr_t>(dst + first) & 15) == 0);
+    for (int32_t c = threadIdx.x; c < chunks; c += 256) {
+      float z[8];
+      const bool whole = load(c, z);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = log_prob(z[i], lse);
+      const int32_t w = first + 8 * c;
+      if (whole && even) {
+        store8(dst + w, z);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (w + i >= lo && w + i < hi) dst[w + i] = z[i];
+      }
+    }
+    if (!slots) return;
+    __syncthreads();  // the named classes' places have been written above, as masked
+    for (int32_t i = threadIdx.x; i < slots; i += 256)
+      if (table[i].id >= 0) dst[table[i].id] = log_prob(table[i].z, lse);
+  }
+};
+
+// One part of a row: its sum, and all the rest where the row has one part.  The
+// parts' sums are kept at part[row][split] = (m, l), the target's z after them.
 template <typename T>
 __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
   __shared__ float zt;
   const int64_t row = blockIdx.x / A.splits;
-  const int32_t split = blockIdx.x % A.splits;
-  const int32_t per = (A.classes + A.splits - 1) / A.splits;
-  const int32_t lo = min(A.classes, split * per), hi = min(A.classes, lo + per);
-  const T* src = static_cast<const T*>(A.logits) + row * A.stride;
-  const uint32_t* mask = mask_of(A, row);
-  const Named N = names(A, row, slots, shared);
+  Part<T> P;
+  if (threadIdx.x == 0) zt = -__builtin_inff();
+  P.start(A, row, blockIdx.x % A.splits, A.splits, slots, shared);
   const int32_t target = A.score ? A.target[row] : -1;
-  Sum s{-__builtin_inff(), 0.0f};
-  for (int32_t w = lo + threadIdx.x; w < hi; w += 256) {
-    const float z = adjusted(A, N, mask, w, as_float(src[w]));
-    add(s, z);
-    if (w == target) zt = z;
-  }
-  s = block_sum(s);  // its barrier also shows zt to all
+  if (!P.sparse) __syncthreads();  // zt
+  Sum s = block_sum(P.sum(target, &zt));  // its barrier also shows zt to all
   if (A.splits > 1) {
-    float* at = A.part + 2 * blockIdx.x;
     if (threadIdx.x == 0) {
-      at[0] = s.m, at[1] = s.l;
-      if (target >= lo && target < hi) A.part[2 * A.rows * A.splits + row] = zt;
+      A.part[2 * static_cast<int64_t>(blockIdx.x)] = s.m;
+      A.part[2 * static_cast<int64_t>(blockIdx.x) + 1] = s.l;
+      if (target >= P.lo && target < P.hi) A.part[2 * A.rows * A.splits + row] = zt;
     }
     return;
   }
   const Lse lse = log_sum(s);
   if (threadIdx.x == 0) finish(A, row, lse, zt);
-  if (!A.logprobs) return;
-  float* dst = A.logprobs + row * A.out_stride;
-  for (int32_t w = lo + threadIdx.x; w < hi; w += 256) {
-    const float z = adjusted(A, N, mask, w, as_float(src[w]));
-    dst[w] = log_prob(z, lse);
-  }
+  if (A.logprobs) P.write(A.logprobs + row * A.out_stride, lse);
 }
 
 // Rows of several parts: joins the sums, then writes the part's log-probabilities.
 template <typename T>
-__global__ __launch_bounds__(256) void k_logits_join(LogitArgs A, int32_t slots, int32_t groups) {
+__global__ __launch_bounds__(256) void k_logits_join(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
-  const int64_t row = blockIdx.x / groups;
-  const int32_t split = blockIdx.x % groups;
+  const int32_t parts = A.logprobs ? A.splits : 1;
+  const int64_t row = blockIdx.x / parts;
+  const int32_t part = blockIdx.x % parts;
   Sum s{-__builtin_inff(), 0.0f};
   for (int32_t k = threadIdx.x; k < A.splits; k += 256) join(s, A.part[2 * (row * A.splits + k)], A.part[2 * (row * A.splits + k) + 1]);
   s = block_sum(s);
   const Lse lse = log_sum(s);
-  if (split == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row]);
+  if (part == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row]);
   if (!A.logprobs) return;
-  const int32_t per = (A.classes + groups - 1) / groups;
-  const int32_t lo = min(A.classes, split * per), hi = min(A.classes, lo + per);
-  const T* src = static_cast<const T*>(A.logits) + row * A.stride;
-  const uint32_t* mask = mask_of(A, row);
-  const Named N = names(A, row, slots, shared);
-  float* dst = A.logprobs + row * A.out_stride;
-  for (int32_t w = lo + threadIdx.x; w < hi; w += 256) {
-    const float z = adjusted(A, N, mask, w, as_float(src[w]));
-    dst[w] = log_prob(z, lse);
+  Part<T> P;
+  P.start(A, row, part, A.splits, slots, shared);
+  P.write(A.logprobs + row * A.out_stride, lse);
+}
+
+// ------------------------------------------------------------------ short rows
+
+// `L` lanes (16 or 64) hold a row: lane i its classes i, i + L, .., E of them.
+// What the row's history and biases say of a class is gathered in LDS, in words
+// of the row's own that are zero before and after.
+template <typename T, int L, int E>
+__global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
+  constexpr int rows = 256 / L;
+  __shared__ int32_t count[rows][L * E], place[rows][L * E];
+  const int at = threadIdx.x / L, lane = threadIdx.x % L;
+  const bool hist = A.r.history_width > 0, biased = A.r.bias_width > 0, own_bias = biased && A.r.bias_per_row;
+  const Rules rules(A.r);
+  float bias[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    bias[e] = 0.0f;
+    count[at][lane + L * e] = place[at][lane + L * e] = 0;
+  }
+  __syncthreads();
+  if (biased && !own_bias) {  // one list for all rows: into registers, once
+    for (int i = lane; i < A.r.bias_width; i += L) {
+      const int32_t id = A.r.bias_ids[i];
+      if (id >= 0 && id < A.classes) atomicMax(&place[at][id], i + 1);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (const int32_t p = place[at][lane + L * e]) bias[e] = A.r.bias_values[p - 1];
+  }
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * rows; r0 < A.rows; r0 += static_cast<int64_t>(gridDim.x) * rows) {
+    const int64_t row = r0 + at;
+    const bool live = row < A.rows;
+    float z[E];
+    const T* src = static_cast<const T*>(A.logits) + row * A.stride;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int32_t w = lane + L * e;
+      z[e] = live && w < A.classes ? as_float(src[w]) : -__builtin_inff();
+    }
+    int32_t n[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) n[e] = 0;
+    if (hist || own_bias) {
+      if (live && hist)
+        for (int i = lane; i < A.r.history_width; i += L) {
+          const int32_t id = A.r.history[row * A.r.history_width + i];
+          if (id >= 0 && id < A.classes) atomicAdd(&count[at][id], 1);
+        }
+      if (live && own_bias)
+        for (int i = lane; i < A.r.bias_width; i += L) {
+          const int32_t id = A.r.bias_ids[row * A.r.bias_width + i];
+          if (id >= 0 && id < A.classes) atomicMax(&place[at][id], i + 1);
+        }
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        n[e] = count[at][lane + L * e];
+        count[at][lane + L * e] = 0;
+        if (own_bias) {
+          const int32_t p = place[at][lane + L * e];
+          bias[e] = p ? A.r.bias_values[row * A.r.bias_width + p - 1] : 0.0f;
+          place[at][lane + L * e] = 0;
+        }
+      }
+      __syncthreads();
+    }
+    const uint32_t* mask = live ? mask_of(A, row) : nullptr;
+    float m = -__builtin_inff();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int32_t w = lane + L * e;
+      z[e] = rules(z[e], n[e], bias[e]);
+      if (w >= A.classes || (mask && !(mask[w >> 5] >> (w & 31) & 1u))) z[e] = -__builtin_inff();
+      m = fmaxf(m, z[e]);
+    }
+    m = over_lanes<L>(m, Max());
+    Sum s{m, 0.0f};
+    const float base = safe(m);
+#pragma unroll
+    for (int e = 0; e < E; ++e) s.l += exp_of(z[e], base);
+    s.l = over_lanes<L>(s.l, Plus());
+    const Lse lse = log_sum(s);
+    if (!live) continue;
+    if (A.lse && lane == 0) A.lse[row] = lse.m + lse.rest;
+    if (A.score) {
+      const int32_t t = A.target[row];
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane + L * e == t && t < A.classes) A.score[row] = log_prob(z[e], lse);
+      if (lane == 0 && (t < 0 || t >= A.classes)) A.score[row] = t < 0 ? 0.0f : __builtin_nanf("");
+    }
+    if (A.logprobs) {
+      float* dst = A.logprobs + row * A.out_stride;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane + L * e < A.classes) dst[lane + L * e] = log_prob(z[e], lse);
+    }
   }
 }
 
+template <typename T, int L, int E>
+hipError_t run_short(const LogitArgs& A, hipStream_t st) {
+  const int64_t groups = (A.rows + 256 / L - 1) / (256 / L);
+  // eight workgroups a CU are resident; more than a few times that only repeats the shared bias list's setup
+  k_logits_short<T, L, E><<<dim3(static_cast<unsigned>(groups < 4096 ? groups : 4096)), 256, 0, st>>>(A);
+  return hipGetLastError();
+}
+
+constexpr int kShortClasses = 512;
+
 template <typename T>
 hipError_t run(const LogitArgs& A, hipStream_t st) {
+  const int32_t C = A.classes;
+  if (C <= 16) return run_short<T, 16, 1>(A, st);
+  if (C <= 32) return run_short<T, 16, 2>(A, st);
+  if (C <= 48) return run_short<T, 16, 3>(A, st);
+  if (C <= 64) return run_short<T, 16, 4>(A, st);
+  if (C <= 128) return run_short<T, 64, 2>(A, st);
+  if (C <= 256) return run_short<T, 64, 4>(A, st);
+  if (C <= kShortClasses) return run_short<T, 64, 8>(A, st);
   const int32_t ids = A.r.history_width + A.r.bias_width;
   int32_t slots = 0;
   if (ids)
     for (slots = 64; slots < 2 * ids; slots <<= 1) {
     }
-  const size_t lds = slots ? kFilterWords * 4 + slots * sizeof(Slot) : 0;
+  const size_t per = (C + A.splits - 1) / A.splits + 8;
+  const size_t lds = slots || A.r.mask ? ((per + 127) / 128 + 1) * 16 + slots * sizeof(Slot) : 0;
   k_logits<T><<<dim3(static_cast<unsigned>(A.rows * A.splits)), 256, lds, st>>>(A, slots);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.splits == 1) return e;
-  const int32_t groups = A.logprobs ? A.splits : 1;
-  k_logits_join<T><<<dim3(static_cast<unsigned>(A.rows * groups)), 256, A.logprobs ? lds : 0, st>>>(A, A.logprobs ? slots : 0, groups);
+  k_logits_join<T><<<dim3(static_cast<unsigned>(A.logprobs ? A.rows * A.splits : A.rows)), 256, A.logprobs ? lds : 0, st>>>(A, slots);
   return hipGetLastError();
 }
 
 }  // namespace
 
+// Parts of a long row: so many that about two workgroups a CU exist, each with
+// 1024 classes at least and kPartClasses at most.
 int32_t logits_splits(int64_t rows, int32_t classes) {
+  if (classes <= kShortClasses) return 1;
   int64_t s = rows > 0 ? (512 + rows - 1) / rows : 1;
   s = s < classes / 1024 ? s : classes / 1024;
-  return static_cast<int32_t>(s < 1 ? 1 : s);
+  const int64_t least = (classes + kPartClasses - 1) / kPartClasses;
+  return static_cast<int32_t>(s < least ? least : s);
 }
 
 hipError_t launch_logits(const LogitArgs& A, int dtype, hipStream_t st) {

@@ -63,7 +63,7 @@ __device__ __forceinline__ int32_t adapter_of(const LoraArgs& A, int64_t row) {
 template <typename T, int RT>
 __global__ __launch_bounds__(256) void k_lora_down(LoraArgs A) {
   using S = Step<T>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, j = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
   const int32_t k_lo = blockIdx.z * A.kspan, k_hi = min(A.d_in, k_lo + A.kspan);
   __shared__ float red[4][RT * 4][64];
@@ -169,7 +169,7 @@ struct Down {
 template <typename T, int RT>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
   using S = Step<T>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, j = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
   const int32_t o_lo = blockIdx.z * kUpChannels + wave * (kUpChannels / 4);
   const int32_t id = adapter_of(A, row);

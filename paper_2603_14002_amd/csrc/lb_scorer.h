@@ -47,6 +47,7 @@ struct AttendArgs {
   float scale2;  // scale * log2(e)
   int32_t window;
   int32_t tiles, splits;
+  bool by_rows;
 };
 
 struct LoraArgs {
@@ -74,9 +75,10 @@ struct LogitArgs {
 // the plan of an attention call: q rows a tile, and the parts a key range is cut into
 struct AttendPlan {
   int32_t tiles, splits;
+  bool by_rows;  // many query rows: wavefronts take rows, else parts of the keys
   int64_t part_floats;
 };
-AttendPlan attend_plan(const KvArgs& kv, int head_dim);
+AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype);  // part_floats is the same for every type
 
 hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st);
@@ -99,6 +101,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// the wavefront's index in its workgroup, in a scalar register: what follows from it is uniform
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 // eight consecutive values from 16-B aligned memory, as 32-bit floats
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {

@@ -202,7 +202,7 @@ lb_status lb_kv_attend_workspace(const lb_kv_cache* cache, const lb_kv_batch* ba
     need(bytes != nullptr, "null host pointer");
     const KvArgs a = kv_args(cache, batch, q_heads);
     check_heads(a);
-    *bytes = a.n_seqs ? attend_plan(a, cache->head_dim).part_floats * 4 : 0;
+    *bytes = a.n_seqs ? attend_plan(a, cache->head_dim, LB_F32).part_floats * 4 : 0;
     return hipSuccess;
   });
 }
@@ -221,9 +221,10 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     check_rows(q, q_stride, width, dtype, rows, "null device pointer: q", "q must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     check_rows(out, out_stride, width, dtype, rows, "null device pointer: out", "out must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     if (rows == 0) return hipSuccess;
-    const AttendPlan p = attend_plan(A.kv, cache->head_dim);
+    const AttendPlan p = attend_plan(A.kv, cache->head_dim, dtype);
     need(static_cast<int64_t>(A.kv.n_seqs) * p.tiles * A.kv.kv_heads * p.splits <= 0x7FFFFFFF,
          "too much work for one call: n_seqs * max_new * q_heads is too large");
+    need(p.splits == 1 || rows * q_heads <= 0x7FFFFFFF, "too much work for one call: n_rows * q_heads is too large");
     need(p.part_floats == 0 || (workspace && aligned(workspace) && workspace_bytes >= p.part_floats * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_kv_attend_workspace says");
     A.q = q;
@@ -236,6 +237,7 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     A.window = window;
     A.tiles = p.tiles;
     A.splits = p.splits;
+    A.by_rows = p.by_rows;
     return launch_kv_attend(A, cache->head_dim, dtype, static_cast<hipStream_t>(stream));
   });
 }

@@ -41,12 +41,15 @@ def close(got, want, bound, what):
     """|got - want| <= bound, and the same infinities and NaN."""
     got = got.detach().cpu().double()
     fine = torch.isfinite(want)
-    assert torch.equal(torch.isnan(got), torch.isnan(want)), what
+    same_nan = torch.equal(torch.isnan(got), torch.isnan(want))
+    assert same_nan, f"{what}: {int(torch.isnan(got).sum())} NaN, {int(torch.isnan(want).sum())} expected"
     inf = ~fine & ~torch.isnan(want)
-    assert torch.equal(got[inf], want[inf]), what
+    same_inf = torch.equal(got[inf], want[inf])
+    assert same_inf, f"{what}: other infinities"
     d = (got - want).abs()[fine]
     b = bound.expand_as(want)[fine] if isinstance(bound, torch.Tensor) else torch.full_like(d, bound)
-    assert bool((d <= b).all()), f"{what}: off by {float(d.max())}, {float((d / b).max())} of the bound"
+    within = bool((d <= b).all())
+    assert within, f"{what}: off by {float(d.max())}, {float((d / b).nan_to_num(0).max())} of the bound, at {int((d > b).sum())} of {d.numel()}"
 
 
 # ------------------------------------------------------------------ append and read
