@@ -1,9 +1,7 @@
 // Low-rank adapters beside a shared projection: out_i = y_i + s_a B_a (A_a x_i).
 //
-// Two launches: the rows' rank-sized products h = A x (summed in 32 bits over
-// parts of d_in, each part's sum kept apart so that the order of addition is
-// fixed), then out = y + s B h.  Both work on 16 rows at a time and, within them,
-// on the distinct adapters one after the other with the other adapters' rows
+// Two launches: the rows' rank-sized products h = A x, kept in 32 bits, then out =
+// y + s B h.  Both work on 16 rows at a time and, within them, on the distinct adapters one after the other with the other adapters' rows
 // held at zero: rows of one request lie together, so a tile mostly has one
 // adapter, and where each row has its own the weights of every row's adapter
 // have to be read anyway.
@@ -58,87 +56,105 @@ __device__ __forceinline__ int32_t adapter_of(const LoraArgs& A, int64_t row) {
   return a >= 0 && a < A.n_adapters ? a : -1;
 }
 
-// h[part][row][rank] for 16 rows and one part of d_in; the wavefronts take every
-// fourth step of it.
+// h[row][rank] for 16 rows: the wavefronts take every W-th piece of d_in and join
+// in LDS.  A piece is two matrix steps: a lane takes 32 adjacent bytes of its
+// row, so that the four lanes of a row read whole lines of 128 B.  U pieces are
+// on their way at a time.
+template <int RT>
+constexpr int kDownWaves = 8;  // 64 KB of LDS at most
+
 template <typename T, int RT>
-__global__ __launch_bounds__(256) void k_lora_down(LoraArgs A) {
+__global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
   using S = Step<T>;
+  constexpr int W = kDownWaves<RT>, U = RT <= 2 ? 4 : 2, KS = 2 * S::KS;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
-  const int32_t k_lo = blockIdx.z * A.kspan, k_hi = min(A.d_in, k_lo + A.kspan);
-  __shared__ float red[4][RT * 4][64];
+  __shared__ float red[W][RT * 4][64];
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   each_adapter(adapter_of(A, row), blockIdx.y, gridDim.y, [&](int32_t a, bool mine) {
-    const T* w = static_cast<const T*>(A.a) + static_cast<int64_t>(a) * A.rank * A.d_in;
+    const T* w = static_cast<const T*>(A.a) + static_cast<int64_t>(a) * A.rank * A.d_in + static_cast<int64_t>(n) * A.d_in;
     f32x4 acc[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[r] = f32x4{0, 0, 0, 0};
-    for (int32_t k0 = k_lo + wave * S::KS; k0 < k_hi; k0 += 4 * S::KS) {
-      const int32_t k = k0 + j * S::W;
-      typename S::V xf{};
-      if (mine && k < k_hi) xf = *reinterpret_cast<const typename S::V*>(x + k);
+    for (int32_t k0 = wave * KS; k0 < A.d_in; k0 += U * W * KS) {
+      typename S::V xf[U][2], wf[U][2][RT];
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        typename S::V wf{};
-        if (r * 16 + n < A.rank && k < k_hi)
-          wf = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(r * 16 + n) * A.d_in + k);
-        acc[r] = S::mul(wf, xf, acc[r]);
-      }
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int32_t k = k0 + u * W * KS + (2 * j + v) * S::W;
+          xf[u][v] = typename S::V{};
+          if (mine && k < A.d_in) xf[u][v] = *reinterpret_cast<const typename S::V*>(x + k);
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            wf[u][v][r] = typename S::V{};
+            if (r * 16 + n < A.rank && k < A.d_in)
+              wf[u][v][r] = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(r * 16) * A.d_in + k);
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+          for (int r = 0; r < RT; ++r) acc[r] = S::mul(wf[u][v][r], xf[u][v], acc[r]);
     }
-    __syncthreads();
+    __syncthreads();  // the last adapter's sums have been read
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
       for (int i = 0; i < 4; ++i) red[wave][4 * r + i][lane] = acc[r][i];
     __syncthreads();
-    if (mine) {
-      float* h = A.h + (static_cast<int64_t>(blockIdx.z) * A.rows + row) * A.rank;
+    for (int at = wave; at < RT * 4; at += W) {
+      float sum = 0.0f;
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        const int at = 4 * r + wave, k = r * 16 + 4 * j + wave;
-        if (k < A.rank) h[k] = red[0][at][lane] + red[1][at][lane] + red[2][at][lane] + red[3][at][lane];
-      }
+      for (int k = 0; k < W; ++k) sum += red[k][at][lane];
+      const int k = (at >> 2) * 16 + 4 * j + (at & 3);
+      if (mine && k < A.rank) A.h[row * A.rank + k] = sum;
     }
   });
 }
 
-constexpr int kUpChannels = 256;  // channels of d_out a workgroup takes: 64 a wavefront, 32 at a time
+constexpr int kUpChannels = 256;  // channels of d_out a workgroup takes: 64 a wavefront
 
-// h as matrix operands.  In 16 bits it goes as its rounding and what that leaves
-// (2^-17 of it for bf16, 2^-22 for fp16), side by side along the summed axis;
-// fp16 is taken relative to the row's largest power of two, so that no h is out
-// of its range.
+// h of a row as matrix operands.  In 16 bits it goes as its rounding and what that
+// leaves (2^-17 of it for bf16, 2^-22 for fp16): two products with the same
+// weights, or, up to rank 16, side by side along the summed axis of one product.
+// fp16 is taken relative to the row's largest power of two, so that no h is out of
+// its range.
 template <typename T, int RT>
 struct Down {
-  typename Step<T>::V v[RT];
+  using S = Step<T>;
+  static constexpr bool wide = sizeof(T) == 4, paired = !wide && RT == 1;
+  static constexpr int N = wide ? RT : paired ? 1 : RT / 2;  // products along the rank
+  static constexpr int pieces = wide || paired ? 1 : 2;
+  typename S::V v[pieces][N];
   float unit;
+
+  // the first of the rank's entries that the lane has in product c (past the rank: none)
+  static __device__ __forceinline__ int32_t entry(int c, int j, int32_t rank) {
+    const int32_t q = c * S::KS + j * S::W;
+    return paired && q >= rank ? (q < 2 * rank ? q - rank : rank) : q;
+  }
+
   __device__ __forceinline__ void load(const LoraArgs& A, int64_t row, bool mine, int j) {
-    const int64_t part = A.rows * static_cast<int64_t>(A.rank);
     const float* h = A.h + row * A.rank;
     unit = 1.0f;
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (wide) {
 #pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        const int k = c * 16 + j * 4;
-        f32x4 x{0, 0, 0, 0};
-        if (mine && k < A.rank)
-          for (int z = 0; z < A.ksplit; ++z) x += *reinterpret_cast<const f32x4*>(h + z * part + k);
-        v[c] = x;
+      for (int c = 0; c < N; ++c) {
+        const int32_t k = entry(c, j, A.rank);
+        v[0][c] = f32x4{0, 0, 0, 0};
+        if (mine && k < A.rank) v[0][c] = *reinterpret_cast<const f32x4*>(h + k);
       }
     } else {
-      float x[RT][8], most = 0.0f;
+      float x[N][8], most = 0.0f;
 #pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        const int q = c * 32 + j * 8, k = q < A.rank ? q : q - A.rank;
+      for (int c = 0; c < N; ++c) {
+        const int32_t k = entry(c, j, A.rank);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[c][i] = 0.0f;
-        if (mine && k < A.rank)
-          for (int z = 0; z < A.ksplit; ++z) {
-            float y[8];
-            load8(h + z * part + k, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[c][i] += y[i];
-          }
+        if (mine && k < A.rank) load8(h + k, x[c]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[c][i]));
       }
@@ -149,17 +165,20 @@ struct Down {
         unit = __uint_as_float(static_cast<uint32_t>(e) << 23);
         const float inv = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
 #pragma unroll
-        for (int c = 0; c < RT; ++c)
+        for (int c = 0; c < N; ++c)
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[c][i] *= inv;
       }
 #pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        const bool low = c * 32 + j * 8 >= A.rank;
+      for (int c = 0; c < N; ++c) {
+        const bool second = paired && c * S::KS + j * S::W >= A.rank;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const T hi = static_cast<T>(x[c][i]);
-          v[c][i] = low ? (__builtin_isinf(x[c][i]) ? T(0.0f) : static_cast<T>(x[c][i] - static_cast<float>(hi))) : hi;
+          // an infinity is one piece: the rest of it would be NaN
+          const T lo = __builtin_isinf(x[c][i]) ? T(0.0f) : static_cast<T>(x[c][i] - static_cast<float>(hi));
+          v[0][c][i] = second ? lo : hi;
+          if constexpr (pieces == 2) v[1][c][i] = lo;
         }
       }
     }
@@ -169,51 +188,73 @@ struct Down {
 template <typename T, int RT>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
   using S = Step<T>;
+  using H = Down<T, RT>;
+  constexpr int G = kUpChannels / 128;  // pairs of 16-channel tiles a wavefront
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
-  const int32_t o_lo = blockIdx.z * kUpChannels + wave * (kUpChannels / 4);
+  const uint32_t chunks = (A.d_out + kUpChannels - 1) / kUpChannels;  // side by side: rows are streamed
+  const int64_t row = static_cast<int64_t>(blockIdx.x / chunks) * 16 + n;
+  const int32_t o_lo = blockIdx.x % chunks * kUpChannels + wave * (kUpChannels / 4);
+  // a lane has the channels o_lo + 8 G j .. + 8 G - 1 of its row: rows are read and written in whole lines
+  const int32_t own = o_lo + 8 * G * j;
+  const T* src = static_cast<const T*>(A.y) + row * A.y_stride + own;
+  T* dst = static_cast<T*>(A.out) + row * A.out_stride + own;
+  float y[G][8];
+  const bool early = gridDim.y == 1 && row < A.rows;  // else the tile's other workgroups would read the row too
+  if (early)
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (own + 8 * g < A.d_out) load8(src + 8 * g, y[g]);
   const int32_t id = adapter_of(A, row);
-  if (blockIdx.y == 0 && id < 0 && row < A.rows && (A.out != A.y)) {
-    for (int32_t o = o_lo + j * 8; o < min(o_lo + kUpChannels / 4, A.d_out); o += 32) {
-      float x[8];
-      load8(static_cast<const T*>(A.y) + row * A.y_stride + o, x);
-      store8(static_cast<T*>(A.out) + row * A.out_stride + o, x);
-    }
-  }
+  if (blockIdx.y == 0 && id < 0 && row < A.rows && A.out != A.y)
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+      if (own + 8 * g < A.d_out) {
+        if (!early) load8(src + 8 * g, y[g]);
+        store8(dst + 8 * g, y[g]);
+      }
   each_adapter(id, blockIdx.y, gridDim.y, [&](int32_t a, bool mine) {
-    Down<T, RT> h;
+    // everything that the lane reads is on its way before the first product
+    const T* w = static_cast<const T*>(A.b) + static_cast<int64_t>(a) * A.d_out * A.rank;
+    typename S::V wf[G][2][H::N];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        // row m of the operand is channel 8 G (m / 4) + 8 g + 4 u + m % 4: a lane gets 8 G adjacent ones
+        const int32_t o = o_lo + (n >> 2) * 8 * G + g * 8 + u * 4 + (n & 3);
+#pragma unroll
+        for (int c = 0; c < H::N; ++c) {
+          const int32_t k = H::entry(c, j, A.rank);
+          wf[g][u][c] = typename S::V{};
+          if (o < A.d_out && k < A.rank) wf[g][u][c] = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(o) * A.rank + k);
+        }
+      }
+    if (!early && mine)
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        if (own + 8 * g < A.d_out) load8(src + 8 * g, y[g]);
+    H h;
     h.load(A, row, mine, j);
     const float scale = (A.scale ? A.scale[a] : 1.0f) * h.unit;
-    const T* w = static_cast<const T*>(A.b) + static_cast<int64_t>(a) * A.d_out * A.rank;
 #pragma unroll
-    for (int g = 0; g < kUpChannels / 128; ++g) {
-      const int32_t o0 = o_lo + g * 32;
-      if (o0 >= A.d_out) break;
+    for (int g = 0; g < G; ++g) {
       f32x4 acc[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        // row m of the operand is channel 8 (m / 4) + 4 u + m % 4, so that a lane gets eight adjacent ones
-        const int32_t o = o0 + (n >> 2) * 8 + u * 4 + (n & 3);
         acc[u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < RT; ++c) {
-          const int q = c * S::KS + j * S::W, k = q < A.rank ? q : q - A.rank;
-          typename S::V wf{};
-          if (o < A.d_out && k < A.rank && (sizeof(T) == 2 || q < A.rank))
-            wf = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(o) * A.rank + k);
-          acc[u] = S::mul(wf, h.v[c], acc[u]);
-        }
+        for (int c = 0; c < H::N; ++c)
+#pragma unroll
+          for (int p = 0; p < H::pieces; ++p) acc[u] = S::mul(wf[g][u][c], h.v[p][c], acc[u]);
       }
-      const int32_t o = o0 + j * 8;
-      if (mine && o < A.d_out) {
-        float x[8];
-        load8(static_cast<const T*>(A.y) + row * A.y_stride + o, x);
+      if (mine && own + 8 * g < A.d_out) {
+        float z[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = fmaf(scale, acc[0][i], x[i]);
-          x[4 + i] = fmaf(scale, acc[1][i], x[4 + i]);
+          z[i] = fmaf(scale, acc[0][i], y[g][i]);
+          z[4 + i] = fmaf(scale, acc[1][i], y[g][4 + i]);
         }
-        store8(static_cast<T*>(A.out) + row * A.out_stride + o, x);
+        store8(dst + 8 * g, z);
       }
     }
   });
@@ -224,11 +265,11 @@ hipError_t run(const LoraArgs& A, hipStream_t st) {
   const unsigned tiles = static_cast<unsigned>((A.rows + 15) / 16);
   const unsigned chunks = static_cast<unsigned>((A.d_out + kUpChannels - 1) / kUpChannels);
   // few tiles: the adapters of a tile side by side
-  const unsigned down = tiles * A.ksplit < 512 ? 16 : 1, up = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
-  k_lora_down<T, RT><<<dim3(tiles, down, static_cast<unsigned>(A.ksplit)), 256, 0, st>>>(A);
+  const unsigned down = tiles < 512 ? 16 : 1, up = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
+  k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves<RT>, 0, st>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_lora_up<T, RT><<<dim3(tiles, up, chunks), 256, 0, st>>>(A);
+  k_lora_up<T, RT><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
@@ -238,15 +279,6 @@ hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
 }
 
 }  // namespace
-
-int32_t lora_ksplit(int64_t rows, int32_t d_in, int32_t* kspan) {
-  const int64_t tiles = (rows + 15) / 16;
-  int64_t s = tiles > 0 ? (512 + tiles - 1) / tiles : 1;
-  s = s < d_in / 256 ? s : d_in / 256;
-  s = s < 1 ? 1 : s > 8 ? 8 : s;
-  *kspan = static_cast<int32_t>(((d_in + s - 1) / s + 127) / 128 * 128);
-  return (d_in + *kspan - 1) / *kspan;
-}
 
 hipError_t launch_lora(const LoraArgs& A, int dtype, hipStream_t st) {
   return dtype == LB_F32 ? by_rank<float>(A, st) : dtype == LB_BF16 ? by_rank<__bf16>(A, st) : by_rank<_Float16>(A, st);

@@ -57,7 +57,7 @@ struct LoraArgs {
   const float* scale;
   float* h;
   int64_t x_stride, y_stride, out_stride;
-  int32_t rows, d_in, d_out, rank, n_adapters, ksplit, kspan;
+  int32_t rows, d_in, d_out, rank, n_adapters;
 };
 
 struct LogitArgs {
@@ -84,8 +84,6 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st);
 
-// parts of d_in that the rows' rank-sized products are summed over, and their length
-int32_t lora_ksplit(int64_t rows, int32_t d_in, int32_t* kspan);
 hipError_t launch_lora(const LoraArgs& A, int dtype, hipStream_t st);
 
 // parts of a row that its sum is taken over (1: no workspace)

@@ -248,8 +248,7 @@ lb_status lb_lora_workspace(int64_t rows, int32_t d_in, int32_t d_out, int32_t r
     need(rows >= 0 && rows <= (1 << 28), "rows must be in 0..2^28");
     need(rank >= 8 && rank <= 128 && rank % 8 == 0, "rank must be a multiple of 8, at most 128");
     need(d_in >= 8 && d_in % 8 == 0 && d_out >= 8 && d_out % 8 == 0, "d_in and d_out must be positive multiples of 8");
-    int32_t kspan;
-    *bytes = rows * rank * lora_ksplit(rows, d_in, &kspan) * 4;
+    *bytes = rows * rank * 4;
     return hipSuccess;
   });
 }
@@ -272,9 +271,9 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     need(aligned(a) && aligned(b), "a and b must be 16-B aligned");
     need(adapter || rows == 0, "null device pointer: adapter");
     if (rows == 0) return hipSuccess;
+    need(((rows + 15) / 16) * ((d_out + 255) / 256) <= (1 << 24), "too much work for one call: rows * d_out is too large");
     LoraArgs A{};
-    A.ksplit = lora_ksplit(rows, d_in, &A.kspan);
-    need(workspace && aligned(workspace) && workspace_bytes >= rows * rank * A.ksplit * 4,
+    need(workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4,
          "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says");
     A.x = x;
     A.y = y;
