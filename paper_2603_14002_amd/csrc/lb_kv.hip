@@ -40,6 +40,11 @@ __device__ __forceinline__ Seq sequence(const KvArgs& A, int32_t s) {
   return q;
 }
 
+// A sequence whose starts or length do not fit is reported by one workgroup, whichever rows it has itself.
+__device__ __forceinline__ void check_sequence(const KvArgs& A, uint32_t s) {
+  if (s < static_cast<uint32_t>(A.n_seqs) && threadIdx.x == 0 && sequence(A, static_cast<int32_t>(s)).bad) raise(A.flags, LB_KV_BAD_LENGTH);
+}
+
 // The page and slot of a token; page < 0: not in the cache's pages.
 __device__ __forceinline__ int64_t page_of(const KvArgs& A, int32_t s, int32_t t) {
   const int32_t p = A.table[static_cast<int64_t>(s) * A.max_pages + (t >> A.page_shift)];
@@ -67,6 +72,24 @@ __device__ __forceinline__ int32_t unit_sequence(const KvArgs& A, int32_t u, int
     lo += k * step;
   }
   *group = u - ((A.starts[lo] >> 2) + 2 * lo);
+  return lo;
+}
+
+// The same for tiles of `per` query rows, `group` to a new token: sequence s owns
+// units starts[s] * group / per + s and on, and has no more tiles than those.
+__device__ __forceinline__ int32_t row_unit(const KvArgs& A, int32_t u, int32_t group, int32_t per, int32_t* tile) {
+  const int lane = threadIdx.x & 63;
+  int32_t lo = 0, n = A.n_seqs;
+  while (n > 1) {
+    const int32_t step = (n + 63) >> 6;
+    const int32_t at = lo + min(lane * step, n - 1);
+    const bool below = lane * step < n && static_cast<int64_t>(A.starts[at]) * group / per + at <= u;
+    const int32_t k = max(1, static_cast<int32_t>(__popcll(__ballot(below)))) - 1;
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  const int64_t t = u - (static_cast<int64_t>(A.starts[lo]) * group / per + lo);
+  *tile = t < -1 || t > 0x7FFFFFFF ? -1 : static_cast<int32_t>(t);
   return lo;
 }
 
@@ -154,7 +177,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
   int32_t group;
   const int32_t s = unit_sequence(A.kv, blockIdx.x, &group);
   const Seq q = sequence(A.kv, s);
-  if (q.bad && group == 0 && blockIdx.y == 0 && threadIdx.x == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+  if (blockIdx.y == 0) check_sequence(A.kv, blockIdx.x);
   const int32_t first = max(q.pos0, 0), last = min(q.pos0 + q.count, q.len);  // positions appended: [first, last)
   const int32_t p4 = ((q.pos0 >> 2) + group) << 2;
   if (group < 0 || group > (q.count >> 2) + 1 || p4 >= last || p4 + 4 <= first) return;
@@ -176,48 +199,63 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
     }
   }
   if (!(live[0] || live[1] || live[2] || live[3])) return;
-  const int64_t row = q.row0 + (p4 - q.pos0);  // row of the unit's first position (not a live one, perhaps)
+  // All loads go before the first store, which they would otherwise have to wait
+  // for (q_out may be q), and have no branch: a position that is not live takes
+  // the data of one that is.
+  int32_t pos[4];
+  int64_t row[4];
+#pragma unroll
+  for (int t = 3; t >= 0; --t) {
+    pos[t] = p4 + (live[t] ? t : live[0] ? 0 : live[1] ? 1 : live[2] ? 2 : 3);
+    row[t] = q.row0 + static_cast<int64_t>(pos[t] - q.pos0);
+  }
   const bool turned = ch < A.rot;
   const int32_t half = A.rot >> 1;
 
   if (kind == 0) {
-    const T* src = static_cast<const T*>(A.q) + head * D;
-    T* dst = static_cast<T*>(A.q_out) + head * D;
+    const T* src = static_cast<const T*>(A.q) + head * D + ch;
+    T* dst = static_cast<T*>(A.q_out) + head * D + ch;
+    // a lane turns both halves of its pairs, and the second half's lanes do nothing: q_out may be q
+    const bool both = turned && !A.interleaved;
+    if (both && ch >= half) return;
+    float x[4][8], y[4][8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (!live[t] || !live_item) continue;
-      const T* x0 = src + (row + t) * A.q_stride;
-      float x[8], r[8];
-      load8(x0 + ch, x);
-      if (!turned) {
-        store8(dst + (row + t) * A.q_out_stride + ch, x);
-        continue;
-      }
-      const int64_t angles = static_cast<int64_t>(p4 + t) * half;
-      if (A.interleaved) {
-        const f32x4 cs = *reinterpret_cast<const f32x4*>(A.cos + angles + ch / 2);
-        const f32x4 sn = *reinterpret_cast<const f32x4*>(A.sin + angles + ch / 2);
+    for (int t = 0; t < 4; ++t) load8(src + row[t] * A.q_stride, x[t]);
+    if (both) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          r[2 * i] = fmaf(x[2 * i], cs[i], -(x[2 * i + 1] * sn[i]));
-          r[2 * i + 1] = fmaf(x[2 * i + 1], cs[i], x[2 * i] * sn[i]);
-        }
-        store8(dst + (row + t) * A.q_out_stride + ch, r);
-      } else if (ch < half) {
-        // a lane turns both halves of its pairs: q_out may be q
-        float y[8], cs[8], sn[8], w[8];
-        load8(x0 + ch + half, y);
-        load8(A.cos + angles + ch, cs);
-        load8(A.sin + angles + ch, sn);
+      for (int t = 0; t < 4; ++t) load8(src + row[t] * A.q_stride + half, y[t]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float cs[8], sn[8];
+        load8(A.cos + static_cast<int64_t>(pos[t]) * half + ch, cs);
+        load8(A.sin + static_cast<int64_t>(pos[t]) * half + ch, sn);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          r[i] = fmaf(x[i], cs[i], -(y[i] * sn[i]));
-          w[i] = fmaf(y[i], cs[i], x[i] * sn[i]);
+          const float a = x[t][i], b = y[t][i];
+          x[t][i] = fmaf(a, cs[i], -(b * sn[i]));
+          y[t][i] = fmaf(b, cs[i], a * sn[i]);
         }
-        store8(dst + (row + t) * A.q_out_stride + ch, r);
-        store8(dst + (row + t) * A.q_out_stride + ch + half, w);
+      }
+    } else if (turned) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const f32x4 cs = *reinterpret_cast<const f32x4*>(A.cos + static_cast<int64_t>(pos[t]) * half + ch / 2);
+        const f32x4 sn = *reinterpret_cast<const f32x4*>(A.sin + static_cast<int64_t>(pos[t]) * half + ch / 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float a = x[t][2 * i], b = x[t][2 * i + 1];
+          x[t][2 * i] = fmaf(a, cs[i], -(b * sn[i]));
+          x[t][2 * i + 1] = fmaf(b, cs[i], a * sn[i]);
+        }
       }
     }
+    if (!live_item) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (live[t]) {
+        store8(dst + row[t] * A.q_out_stride, x[t]);
+        if (both) store8(dst + row[t] * A.q_out_stride + half, y[t]);
+      }
     return;
   }
 
@@ -230,44 +268,47 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
   }
   uint8_t* block = A.kv.pages + (page * A.kv.kv_heads + h) * (static_cast<int64_t>(P) * (D + D / 16));
   const int32_t slot = p4 & (P - 1);
-  uint32_t codes[4] = {0, 0, 0, 0};
-  int32_t scale[4] = {0, 0, 0, 0};
+  uint32_t codes[4];
+  int32_t scale[4];
   if (kind == 1) {
-    const T* src = static_cast<const T*>(A.k) + h * D;
+    const T* src = static_cast<const T*>(A.k) + h * D + ch;
+    float x[4][8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      double r[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (live[t]) {
-        const T* x0 = src + (row + t) * A.k_stride;
-        float x[8];
-        load8(x0 + ch, x);
-        const int64_t angles = static_cast<int64_t>(p4 + t) * half;
+    for (int t = 0; t < 4; ++t) load8(src + row[t] * A.k_stride, x[t]);
+    if ((ch & ~31) >= A.rot) {  // the whole block stays: the four lanes of a block go the same way
+#pragma unroll
+      for (int t = 0; t < 4; ++t) value_block(x[t], codes[t], scale[t]);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        double r[8];
+        const int64_t angles = static_cast<int64_t>(pos[t]) * half;
         if (!turned) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) r[i] = x[i];
+          for (int i = 0; i < 8; ++i) r[i] = x[t][i];
         } else if (A.interleaved) {
           const f32x4 cs = *reinterpret_cast<const f32x4*>(A.cos + angles + ch / 2);
           const f32x4 sn = *reinterpret_cast<const f32x4*>(A.sin + angles + ch / 2);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const double a = x[2 * i], b = x[2 * i + 1], c0 = cs[i], s0 = sn[i];
+            const double a = x[t][2 * i], b = x[t][2 * i + 1], c0 = cs[i], s0 = sn[i];
             r[2 * i] = fma(a, c0, -(b * s0));
             r[2 * i + 1] = fma(b, c0, a * s0);
           }
         } else {
           float y[8], cs[8], sn[8];
           const bool low = ch < half;
-          load8(x0 + (low ? ch + half : ch - half), y);
+          load8(src + row[t] * A.k_stride + (low ? half : -half), y);
           load8(A.cos + angles + (low ? ch : ch - half), cs);
           load8(A.sin + angles + (low ? ch : ch - half), sn);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const double b = static_cast<double>(y[i]) * static_cast<double>(sn[i]);
-            r[i] = fma(static_cast<double>(x[i]), static_cast<double>(cs[i]), low ? -b : b);
+            r[i] = fma(static_cast<double>(x[t][i]), static_cast<double>(cs[i]), low ? -b : b);
           }
         }
+        key_block(r, codes[t], scale[t]);
       }
-      key_block(r, codes[t], scale[t]);
     }
     if (!live_item) return;
 #pragma unroll
@@ -278,13 +319,12 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
     }
     return;
   }
-  const T* src = static_cast<const T*>(A.v) + h * D;
+  const T* src = static_cast<const T*>(A.v) + h * D + ch;
+  float x[4][8];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (live[t]) load8(src + (row + t) * A.v_stride + ch, x);
-    value_block(x, codes[t], scale[t]);
-  }
+  for (int t = 0; t < 4; ++t) load8(src + row[t] * A.v_stride, x[t]);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) value_block(x[t], codes[t], scale[t]);
   if (!live_item) return;
   uint8_t* at = block + P * D / 2 + ((slot >> 2) * (D / 2) + c * 4) * 4;
   uint8_t* scale_at = block + P * D + P * D / 32 + ((slot >> 2) * (D / 32) + (c >> 2)) * 4;
@@ -316,7 +356,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
   int32_t group;
   const int32_t s = unit_sequence(A.kv, blockIdx.x, &group);
   const Seq q = sequence(A.kv, s);
-  if (q.bad && group == 0 && blockIdx.y == 0 && threadIdx.x == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+  if (blockIdx.y == 0) check_sequence(A.kv, blockIdx.x);
   const int32_t first = max(q.pos0, 0), last = min(q.pos0 + q.count, q.len);
   const int32_t p4 = ((q.pos0 >> 2) + group) << 2;
   if (group < 0 || group > (q.count >> 2) + 1 || p4 >= last || p4 + 4 <= first) return;
@@ -382,9 +422,9 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
 //
 // Scores, maxima, sums and outputs are held in 32 bits.  The matrix operands are
 // bf16: keys and values exactly; queries and probabilities in `NP` pieces, each
-// the rounding of what the ones before leave: one piece (relative error 2^-9 of a
-// probability) for bf16, whose output has that rounding anyway, two (2^-17) for
-// fp16, three (2^-25) for fp32.  bf16 queries are exact with one, fp16 ones with two.
+// the rounding of what the ones before leave: one piece (off by at most 2^-8 of a
+// probability) for bf16, whose output has that rounding anyway, two (2^-16) for
+// fp16, three (2^-24) for fp32.  bf16 queries are exact with one, fp16 ones with two.
 
 template <typename T>
 struct Pieces;
@@ -445,41 +485,21 @@ __device__ __forceinline__ uint32_t bytes_255(uint32_t w) {
   return (all >> 7) * 255u;
 }
 
-// A tile (32 tokens) in the cache's form, by halves of 16 tokens.
-template <int D>
-struct Tile {
-  uint32_t k[2][D / 32];  // D/4 codes: the lane's quarter of key n
-  uint32_t v[2][D / 32];  // values of tokens 4 j .. 4 j + 3, channel pairs D/32 n .. D/32 (n + 1) - 1
-  uint32_t ks[2];         // scale bytes of the quarter's blocks (one, or two with D = 256)
-  uint32_t vs[2];         // scale bytes of the four tokens' values
-};
-
-// The key range of a wavefront: tiles of 32 tokens from `begin` on, every
-// `step`-th of them.  Lane i holds the pages of the i-th of the next 64 tiles, so
-// a tile's address needs no load before it.
-template <int D>
-struct Keys {
-  const uint8_t* base;   // head h of page 0
-  int64_t page_bytes;
+// The pages of a key range: tiles of 32 tokens from `begin` on, of which a
+// wavefront takes every `step`-th.  Lane i holds the pages (of both halves of 16
+// tokens) of the i-th of the next 64 tiles, so a tile's address needs no load
+// before it.
+struct Pages {
   const int32_t* table;
   int32_t n_pages, shift, begin, end, step;
   static constexpr int32_t kNothing = -(1 << 29);  // no tile is within 64 steps of it
   int32_t held, page0, page1;
-  uint32_t k_at, v_at, ks_at, vs_at;
 
-  __device__ __forceinline__ Keys(const KvArgs& A, int32_t s, int32_t h, int32_t begin_, int32_t end_, int32_t step_, int n, int j)
+  __device__ __forceinline__ Pages(const KvArgs& A, int32_t s, int32_t begin_, int32_t end_, int32_t step_)
       : table(A.table + static_cast<int64_t>(s) * A.max_pages), n_pages(static_cast<int32_t>(A.n_pages)), shift(A.page_shift),
-        begin(begin_), end(end_), step(step_), held(kNothing), page0(-1), page1(-1) {
-    const int32_t P = 1 << shift, block = P * (D + D / 16);
-    base = A.pages + static_cast<int64_t>(h) * block;
-    page_bytes = static_cast<int64_t>(block) * A.kv_heads;
-    k_at = n * (D / 2) + j * (D / 8);
-    v_at = P * (D / 2) + j * (D * 2) + n * (D / 8);
-    ks_at = P * D + n * (D / 32) + j * D / 128;
-    vs_at = P * D + P * (D / 32) + (j * (D / 32) + n * D / 512) * 4;
-  }
+        begin(begin_), end(end_), step(step_), held(kNothing), page0(-1), page1(-1) {}
 
-  // makes lane i hold the pages of tile t + i * step, if tile `t` has left what is held
+  // makes lane i hold the pages of tile t + i * step
   __device__ __forceinline__ void hold(int32_t t, uint32_t* flags) {
     const int lane = threadIdx.x & 63;
     held = t;
@@ -493,39 +513,131 @@ struct Keys {
     }
   }
 
-  // loads tile t; bit u of the result: half u exists
-  __device__ __forceinline__ int load(int32_t t, Tile<D>& X, uint32_t* flags) {
+  // the pages of tile t's halves, -1: none
+  __device__ __forceinline__ void of(int32_t t, int32_t (&page)[2], uint32_t* flags) {
     int32_t i = (t - held) / step;
     if (i >= 64 || i < 0) {
       hold(t, flags);
       i = 0;
     }
+    page[0] = __builtin_amdgcn_readlane(page0, i);
+    page[1] = __builtin_amdgcn_readlane(page1, i);
+  }
+  __device__ __forceinline__ int32_t slot(int32_t t, int u) const { return (begin + t * 32 + 16 * u) & ((1 << shift) - 1); }
+};
+
+// N words from memory that is aligned to as many (2 or 4: in one load)
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+  if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const u32x2 a = *reinterpret_cast<const u32x2*>(p);
+    w[0] = a.x, w[1] = a.y;
+  } else {
+#pragma unroll
+    for (int c = 0; c < N; c += 4) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(p + 4 * c);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[c + x] = a[x];
+    }
+  }
+}
+
+// A tile (32 tokens) in the cache's form, by halves of 16 tokens.
+template <int D>
+struct Tile {
+  uint32_t k[2][D / 32];  // D/4 codes: the lane's quarter of key n
+  uint32_t v[2][D / 32];  // values of tokens 4 j .. 4 j + 3, channel pairs D/32 n .. D/32 (n + 1) - 1
+  uint32_t ks[2];         // scale bytes of the quarter's blocks (one, or two with D = 256)
+  uint32_t vs[2];         // scale bytes of the four tokens' values
+};
+
+// A wavefront's whole tiles of one KV head.
+template <int D>
+struct Keys {
+  Pages P;
+  const uint8_t* base;  // the head's part of page 0
+  int64_t page_bytes;
+  uint32_t k_at, v_at, ks_at, vs_at;
+
+  __device__ __forceinline__ Keys(const KvArgs& A, int32_t s, int32_t h, int32_t begin, int32_t end, int32_t step, int n, int j)
+      : P(A, s, begin, end, step) {
+    const int32_t T = 1 << A.page_shift, block = T * (D + D / 16);
+    base = A.pages + static_cast<int64_t>(h) * block;
+    page_bytes = static_cast<int64_t>(block) * A.kv_heads;
+    k_at = n * (D / 2) + j * (D / 8);
+    v_at = T * (D / 2) + j * (D * 2) + n * (D / 8);
+    ks_at = T * D + n * (D / 32) + j * D / 128;
+    vs_at = T * D + T * (D / 32) + (j * (D / 32) + n * D / 512) * 4;
+  }
+
+  // loads tile t; bit u of the result: half u exists
+  __device__ __forceinline__ int load(int32_t t, Tile<D>& X, uint32_t* flags) {
+    int32_t page[2];
+    P.of(t, page, flags);
     int ok = 0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int32_t page = __builtin_amdgcn_readlane(u ? page1 : page0, i);
-      if (page < 0) continue;  // what the registers hold stays unseen
+      if (page[u] < 0) continue;  // what the registers hold stays unseen
       ok |= 1 << u;
-      const int32_t slot = (begin + t * 32 + 16 * u) & ((1 << shift) - 1);
-      const uint8_t* at = base + page * page_bytes + slot * (D / 2);
-      const uint8_t* scales = base + page * page_bytes + slot * (D / 32);
-      if constexpr (D == 64) {
-        const u32x2 a = *reinterpret_cast<const u32x2*>(at + k_at), b = *reinterpret_cast<const u32x2*>(at + v_at);
-        X.k[u][0] = a.x, X.k[u][1] = a.y, X.v[u][0] = b.x, X.v[u][1] = b.y;
-      } else {
-#pragma unroll
-        for (int c = 0; c < D / 128; ++c) {
-          const u32x4 a = *reinterpret_cast<const u32x4*>(at + k_at + 16 * c), b = *reinterpret_cast<const u32x4*>(at + v_at + 16 * c);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) X.k[u][4 * c + x] = a[x], X.v[u][4 * c + x] = b[x];
-        }
-      }
+      const int32_t slot = P.slot(t, u);
+      const uint8_t* at = base + page[u] * page_bytes + slot * (D / 2);
+      const uint8_t* scales = base + page[u] * page_bytes + slot * (D / 32);
+      load_words<D / 32>(at + k_at, X.k[u]);
+      load_words<D / 32>(at + v_at, X.v[u]);
       X.ks[u] = D == 256 ? *reinterpret_cast<const uint16_t*>(scales + ks_at) : scales[ks_at];
       X.vs[u] = *reinterpret_cast<const uint32_t*>(scales + vs_at);
     }
     return ok;
   }
 };
+
+// The values' scales of a tile, tokens from `end` on (and of halves that do not
+// exist) as 0, whatever the cache holds there, and blocks of NaN too: what is NaN
+// is left in `nan`, 255 a byte.
+struct ValueScales {
+  uint32_t bytes[2], nan[2];
+  float s[2][4];
+
+  __device__ __forceinline__ ValueScales(const uint32_t (&vs)[2], int32_t tb, int32_t end, int ok, int j) {
+    bytes[0] = vs[0], bytes[1] = vs[1];
+    if (ok != 3 || tb + 32 > end) {
+      asm volatile("");  // a branch: most tiles are whole
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int32_t left = ok >> u & 1 ? end - (tb + 16 * u + 4 * j) : 0;
+        bytes[u] = left >= 4 ? bytes[u] : left <= 0 ? 0u : bytes[u] & ((1u << (8 * left)) - 1u);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      nan[u] = bytes_255(bytes[u]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[u][i] = scale_of((bytes[u] & ~nan[u]) >> (8 * i) & 255u);
+    }
+  }
+  __device__ __forceinline__ bool any_nan() const { return __any((nan[0] | nan[1]) != 0); }
+
+  // one word of values (a channel pair of four tokens) of each half, as bf16: [half][token] channel pairs
+  __device__ __forceinline__ void convert(uint32_t w0, uint32_t w1, uint32_t (&y)[2][4]) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t w = u ? w1 : w0;
+      y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][0], 0));
+      y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][1], 1));
+      y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][2], 2));
+      y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][3], 3));
+    }
+  }
+};
+// the even (odd: 1) channel of the pairs for the eight tokens
+__device__ __forceinline__ bf16x8 channel(const uint32_t (&y)[2][4], int odd) {
+  const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+  const u32x4 f{__builtin_amdgcn_perm(y[0][1], y[0][0], sel), __builtin_amdgcn_perm(y[0][3], y[0][2], sel),
+                __builtin_amdgcn_perm(y[1][1], y[1][0], sel), __builtin_amdgcn_perm(y[1][3], y[1][2], sel)};
+  return __builtin_bit_cast(bf16x8, f);
+}
 
 // The state of QT tiles of 16 query rows in one wavefront.
 template <int D, int NP, int QT>
@@ -542,26 +654,30 @@ struct Rows {
   // exp2 keep their precision, and most tiles need no exchange between lanes.
   static constexpr float kSlack = 8.0f;
 
-  // One tile of keys and values.  edge: some row does not see some of its tokens.
-  __device__ __forceinline__ void take(const Tile<D>& X, int32_t tb, int ok, bool edge, int j) {
+  // every row sees the whole tile at tb
+  __device__ __forceinline__ bool inner(int32_t tb, int ok) const {
+    return ok == 3 && tb + 31 <= p_min && tb + 32 <= end && (window <= 0 || tb > p_max - window);
+  }
+
+  // The probabilities of a tile's tokens as matrix operands, and their sums.
+  // key(u, c): channels j D/4 + 8 c .. + 7 of the lane's token in half u.
+  template <typename Key>
+  __device__ __forceinline__ void weigh(Key&& key, int32_t tb, int ok, int j, bf16x8 (&pf)[QT][NP]) {
     f32x4 acc[QT][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      bf16x8 kf[KC];
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
-        // channels j D/4 + 8 c .. + 7 lie in block (8 c) / 32 of the quarter (D = 256 has two there)
-        kf[c] = bf16_of(X.k[u][c], scale_of(D == 256 ? (X.ks[u] >> (c < KC / 2 ? 0 : 8)) & 255u : X.ks[u]));
+      for (int t = 0; t < QT; ++t) acc[t][u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        acc[t][u] = f32x4{0, 0, 0, 0};
+      for (int c = 0; c < KC; ++c) {
+        const bf16x8 kf = key(u, c);
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int p = 0; p < NP; ++p) acc[t][u] = mfma(kf[c], q[t][c][p], acc[t][u]);
+          for (int p = 0; p < NP; ++p) acc[t][u] = mfma(kf, q[t][c][p], acc[t][u]);
       }
     }
-    if (edge) {
+    if (!inner(tb, ok)) {
       asm volatile("");  // a branch: most tiles are whole
 #pragma unroll
       for (int t = 0; t < QT; ++t)
@@ -571,7 +687,6 @@ struct Rows {
           for (int i = 0; i < 4; ++i)
             if (!seen(t, tb + 16 * u + 4 * j + i, ok >> u & 1)) acc[t][u][i] = -__builtin_inff();
     }
-    bf16x8 pf[QT][NP];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float top = larger(larger(larger(acc[t][0][0], acc[t][0][1]), larger(acc[t][0][2], acc[t][0][3])),
@@ -594,48 +709,34 @@ struct Rows {
       }
       split8<NP>(p, pf[t]);
     }
+  }
 
-    // the values' scales; tokens that no row sees count as 0, whatever the cache
-    // holds there, and blocks of NaN too at first
-    uint32_t bytes[2] = {X.vs[0], X.vs[1]};
-    if (edge) {
-      asm volatile("");
+  // o += p times channel operand c of the tile's values
+  __device__ __forceinline__ void add_channel(int c, bf16x8 vf, const bf16x8 (&pf)[QT][NP]) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int32_t left = ok >> u & 1 ? end - (tb + 16 * u + 4 * j) : 0;
-        bytes[u] = left >= 4 ? bytes[u] : left <= 0 ? 0u : bytes[u] & ((1u << (8 * left)) - 1u);
-      }
-    }
-    float vs[2][4];
-    const uint32_t nan[2] = {bytes_255(bytes[0]), bytes_255(bytes[1])};
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vs[u][i] = scale_of((bytes[u] & ~nan[u]) >> (8 * i) & 255u);
+      for (int p = 0; p < NP; ++p) o[t][c] = mfma(vf, pf[t][p], o[t][c]);
+  }
+
+  // One tile of keys and values.
+  __device__ __forceinline__ void take(const Tile<D>& X, int32_t tb, int ok, int j) {
+    bf16x8 pf[QT][NP];
+    weigh(
+        [&](int u, int c) {
+          // channels j D/4 + 8 c .. + 7 lie in block (8 c) / 32 of the quarter (D = 256 has two there)
+          return bf16_of(X.k[u][c], scale_of(D == 256 ? (X.ks[u] >> (c < KC / 2 ? 0 : 8)) & 255u : X.ks[u]));
+        },
+        tb, ok, j, pf);
+    const ValueScales V(X.vs, tb, end, ok, j);
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {
       uint32_t y[2][4];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][0], 0));
-        y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][1], 1));
-        y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][2], 2));
-        y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(X.v[u][w], vs[u][3], 3));
-      }
-#pragma unroll
-      for (int par = 0; par < 2; ++par) {
-        // the even (odd) channel of the pair for the eight tokens
-        const uint32_t sel = par ? 0x07060302u : 0x05040100u;
-        const u32x4 f{__builtin_amdgcn_perm(y[0][1], y[0][0], sel), __builtin_amdgcn_perm(y[0][3], y[0][2], sel),
-                      __builtin_amdgcn_perm(y[1][1], y[1][0], sel), __builtin_amdgcn_perm(y[1][3], y[1][2], sel)};
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, f);
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-          for (int p = 0; p < NP; ++p) o[t][2 * w + par] = mfma(vf, pf[t][p], o[t][2 * w + par]);
-      }
+      V.convert(X.v[0][w], X.v[1][w], y);
+      add_channel(2 * w, channel(y, 0), pf);
+      add_channel(2 * w + 1, channel(y, 1), pf);
     }
-    if (__any((nan[0] | nan[1]) != 0)) spread_nan(nan, tb, ok, j);
+    if (V.any_nan()) spread_nan(V.nan, tb, ok, j);
   }
 
   __device__ __forceinline__ bool seen(int t, int32_t tok, bool ok) const {
@@ -669,12 +770,9 @@ struct Rows {
   __device__ __forceinline__ void sweep(Keys<D>& K, int32_t t, int32_t t_hi, int j, uint32_t* flags) {
     Tile<D> X{}, Y{};
     int ok = t < t_hi ? K.load(t, X, flags) : 0;
-    for (; t < t_hi; t += K.step) {
-      const int next = t + K.step < t_hi ? K.load(t + K.step, Y, flags) : 0;
-      const int32_t tb = K.begin + t * 32;
-      // every row sees the whole tile
-      const bool inner = ok == 3 && tb + 31 <= p_min && tb + 32 <= end && (window <= 0 || tb > p_max - window);
-      take(X, tb, ok, !inner, j);
+    for (; t < t_hi; t += K.P.step) {
+      const int next = t + K.P.step < t_hi ? K.load(t + K.P.step, Y, flags) : 0;
+      take(X, K.P.begin + t * 32, ok, j);
       X = Y;
       ok = next;
     }
@@ -685,26 +783,30 @@ struct Rows {
 // spilling (o and q take 4 D/16 + 4 D/32 NP registers a row tile).
 constexpr int waves(int D, int pieces, int QT) { return D * QT * (1 + pieces) <= 256 ? 3 : D * QT * (1 + pieces) <= 768 ? 2 : 1; }
 
+constexpr int kFewRows = 64;      // query rows of a sequence and KV head that the few-row kernel takes
+constexpr int kMostSplits = 128;  // parts of a key range
+
 // query row tiles of 16 a wavefront holds where there are many rows
 __host__ __device__ constexpr int row_tiles(int D, int pieces) { return D * (1 + pieces) <= 384 ? 2 : 1; }
 
-// What a workgroup has to do: rows r0 .. of a sequence and KV head.
+// What a workgroup has to do: a tile of the query rows of a sequence and KV head.
+// Row r is new token r / G and query head r % G of those that share the KV head.
 struct Job {
   Seq q;
-  int32_t s, h, tile, split, G, R;
+  int32_t s, h, tile, G, R;
 };
-__device__ __forceinline__ Job job_of(const AttendArgs& A) {
+
+// The job of the few-row kernel: tile `rest % tiles` of head h of sequence s.
+__device__ __forceinline__ Job few_job(const AttendArgs& A, uint32_t job) {
   Job w;
-  w.split = blockIdx.x % A.splits;
-  uint32_t rest = blockIdx.x / A.splits;
-  w.h = static_cast<int32_t>(rest % A.kv.kv_heads);
-  rest /= A.kv.kv_heads;
-  w.s = static_cast<int32_t>(rest / A.tiles);
-  w.tile = A.tiles - 1 - static_cast<int32_t>(rest % A.tiles);  // the last rows see most keys: they go first
+  w.tile = static_cast<int32_t>(job % A.tiles);
+  job /= A.tiles;
+  w.h = static_cast<int32_t>(job % A.kv.kv_heads);
+  w.s = static_cast<int32_t>(job / A.kv.kv_heads);
   w.q = sequence(A.kv, w.s);
-  if (w.q.bad && w.tile == 0 && w.h == 0 && w.split == 0 && threadIdx.x == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
   w.G = A.kv.q_heads / A.kv.kv_heads;
   w.R = w.q.count * w.G;
+  if (w.R > kFewRows) w.R = 0;  // the many-row kernel's
   return w;
 }
 
@@ -768,14 +870,17 @@ template <int D, typename T>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  const Job w = job_of(A);
+  check_sequence(A.kv, blockIdx.x);
+  const uint32_t job = blockIdx.x / A.splits;
+  const int32_t split = static_cast<int32_t>(blockIdx.x % A.splits);
+  const Job w = few_job(A, job);
   Rows<D, Pieces<T>::n, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
   const int32_t tiles = S.end > begin ? (S.end - begin + 31) >> 5 : 0;
   const int32_t per = (tiles + A.splits - 1) / A.splits;
   Keys<D> K(A.kv, w.s, w.h, begin, S.end, 4, n, j);
-  S.sweep(K, w.split * per + wave, min(tiles, (w.split + 1) * per), j, A.kv.flags);
+  S.sweep(K, split * per + wave, min(tiles, (split + 1) * per), j, A.kv.flags);
   const float l = row_sum(S.l[0]);
 
   // join the four wavefronts
@@ -809,11 +914,11 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
     for (int k = 0; k < 4; ++k) x[c] += wgt[k] * part[k][4 * c + i][lane];
   }
   const int32_t ch = (4 * j + i) * (D / 16);
-  const int64_t at = row * A.kv.q_heads + hq;
   if (A.splits > 1) {
-    store_channels<VC>(A.part + (at * A.splits + w.split) * D + ch, x);
+    const int64_t at = (static_cast<int64_t>(job) * A.part_rows + n) * A.splits + split;
+    store_channels<VC>(A.part + at * D + ch, x);
     if (i == 0 && j == 0) {
-      float* sums = A.part + static_cast<int64_t>(A.kv.n_rows) * A.kv.q_heads * A.splits * D + (at * A.splits + w.split) * 2;
+      float* sums = A.part + A.part_sums + at * 2;
       sums[0] = M, sums[1] = L;
     }
     return;
@@ -822,26 +927,151 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
 #pragma unroll
   for (int c = 0; c < VC; ++c) x[c] *= inv;
   store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + ch, x);
-  if (A.lse && i == 0 && j == 0) A.lse[at] = lse_of(base, L);
+  if (A.lse && i == 0 && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(base, L);
 }
 
-// Many query rows: each of the four wavefronts takes 16 QT rows of its own and
-// walks all keys that these see.
+// Many query rows: each of the four wavefronts has 16 QT rows of its own, and all
+// take the same tiles.  A tile is converted to bf16 operands once, a quarter by
+// each wavefront, and goes through LDS in the order in which lanes read it; the
+// conversion of the next one and the loads of the one after it are made while a
+// tile is used, with one barrier a tile.
+template <int D>
+struct Shared {
+  static constexpr int KC = D / 32, VC = D / 16;
+  bf16x8 key[2][2 * KC][64], value[2][VC][64];  // [tile % 2][half and channels, or channel][lane]
+  uint32_t nan[2][2][64];
+  int32_t any_nan[2];
+};
+
+template <int D>
+struct Maker {
+  static constexpr int F = D / 64, W = F > 1 ? F / 2 : 1;  // operands of keys and of values a wavefront makes; words of values
+  Pages P;
+  const uint8_t* base;
+  int64_t page_bytes;
+  uint32_t k_at, v_at, ks_at, vs_at;
+  int u;  // the half whose keys are this wavefront's
+  uint32_t k[F], v[2][W], ks, vs[2];
+  int ok;
+
+  __device__ __forceinline__ Maker(const KvArgs& A, int32_t s, int32_t h, int32_t begin, int32_t end, int wave, int n, int j)
+      : P(A, s, begin, end, 1), u(wave >> 1), ks(0), ok(0) {
+    const int32_t T = 1 << A.page_shift, block = T * (D + D / 16), c0 = (wave & 1) * F, w0 = D == 64 ? wave >> 1 : wave * W;
+    base = A.pages + static_cast<int64_t>(h) * block;
+    page_bytes = static_cast<int64_t>(block) * A.kv_heads;
+    k_at = n * (D / 2) + j * (D / 8) + c0 * 4;
+    v_at = T * (D / 2) + j * (D * 2) + n * (D / 8) + w0 * 4;
+    ks_at = T * D + n * (D / 32) + (j * (D / 4) + c0 * 8) / 32;
+    vs_at = T * D + T * (D / 32) + (j * (D / 32) + n * D / 512) * 4;
+#pragma unroll
+    for (int i = 0; i < F; ++i) k[i] = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[0][i] = v[1][i] = 0;
+    vs[0] = vs[1] = 0;
+  }
+
+  __device__ __forceinline__ void load(int32_t t, uint32_t* flags) {
+    int32_t page[2];
+    P.of(t, page, flags);
+    ok = (page[0] >= 0 ? 1 : 0) | (page[1] >= 0 ? 2 : 0);
+    if (const int32_t mine = u ? page[1] : page[0]; mine >= 0) {
+      const uint8_t* at = base + mine * page_bytes;
+      load_words<F>(at + P.slot(t, u) * (D / 2) + k_at, k);
+      ks = at[P.slot(t, u) * (D / 32) + ks_at];
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      if (page[x] < 0) continue;
+      const uint8_t* at = base + page[x] * page_bytes;
+      load_words<W>(at + P.slot(t, x) * (D / 2) + v_at, v[x]);
+      vs[x] = *reinterpret_cast<const uint32_t*>(at + P.slot(t, x) * (D / 32) + vs_at);
+    }
+  }
+
+  // what has been loaded, into buffer b; tb: the tile's first token
+  __device__ __forceinline__ void make(Shared<D>& L, int b, int32_t tb, int wave, int lane) const {
+    const float s = scale_of(ks);
+#pragma unroll
+    for (int i = 0; i < F; ++i) L.key[b][wave * F + i][lane] = bf16_of(k[i], s);
+    const ValueScales V(vs, tb, P.end, ok, lane >> 4);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      uint32_t y[2][4];
+      V.convert(v[0][i], v[1][i], y);
+      if constexpr (D == 64) {
+        L.value[b][wave][lane] = channel(y, wave & 1);
+      } else {
+        L.value[b][wave * F + 2 * i][lane] = channel(y, 0);
+        L.value[b][wave * F + 2 * i + 1][lane] = channel(y, 1);
+      }
+    }
+    if (wave == 0) {  // its lanes have the scales of all blocks
+      const bool any = V.any_nan();
+      if (any) L.nan[b][0][lane] = V.nan[0], L.nan[b][1][lane] = V.nan[1];
+      if (lane == 0) L.any_nan[b] = any;
+    }
+  }
+};
+
 template <int D, typename T, int QT>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows(AttendArgs A) {
-  constexpr int VC = D / 16;
+  constexpr int VC = D / 16, NP = Pieces<T>::n, per = 64 * QT;
+  __shared__ Shared<D> L;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  const Job w = job_of(A);
-  Rows<D, Pieces<T>::n, QT> S;
-  const int32_t r0 = (w.tile * 4 + wave) * 16 * QT;
-  if (!rows_of<D, T, QT>(A, w, r0, S, n, j)) return;
-  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
-  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
-  S.sweep(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
+  check_sequence(A.kv, blockIdx.x);
+  Job w;
+  w.G = A.kv.q_heads / A.kv.kv_heads;
+  w.h = static_cast<int32_t>(blockIdx.x % A.kv.kv_heads);
+  w.s = row_unit(A.kv, static_cast<int32_t>(blockIdx.x / A.kv.kv_heads), w.G, per, &w.tile);
+  w.q = sequence(A.kv, w.s);
+  w.R = w.q.count * w.G;
+  if (A.few && w.R <= kFewRows) return;  // the few-row kernel's
+  const int32_t tiles_of_rows = (w.R + per - 1) / per;
+  if (w.tile < 0 || w.tile >= tiles_of_rows) return;
+  w.tile = tiles_of_rows - 1 - w.tile;  // the last rows see most keys: they go first
+  Rows<D, NP, QT> S;
+  const bool have = rows_of<D, T, QT>(A, w, (w.tile * 4 + wave) * 16 * QT, S, n, j);
+  // the key range of all four wavefronts' rows
+  const int32_t first = w.q.pos0 + w.tile * per / w.G, last = w.q.pos0 + (min(w.R, (w.tile + 1) * per) - 1) / w.G;
+  const int32_t begin = A.window > 0 ? max(0, first - A.window + 1) & ~31 : 0, end = min(w.q.len, last + 1);
+  const int32_t tiles = end > begin ? (end - begin + 31) >> 5 : 0;
+  Maker<D> M(A.kv, w.s, w.h, begin, end, wave, n, j);
+  int ok = 0;
+  if (tiles > 0) {
+    M.load(0, A.kv.flags);
+    M.make(L, 0, begin, wave, lane);
+    ok = M.ok;
+    if (tiles > 1) M.load(1, A.kv.flags);
+  }
+  __syncthreads();
+  for (int32_t t = 0; t < tiles; ++t) {
+    const int b = t & 1;
+    const int32_t tb = begin + t * 32;
+    int next = 0;
+    if (t + 1 < tiles) {
+      M.make(L, b ^ 1, tb + 32, wave, lane);
+      next = M.ok;
+      if (t + 2 < tiles) M.load(t + 2, A.kv.flags);
+    }
+    // a row of this wavefront may see the tile
+    if (have && tb <= S.p_max && (S.window <= 0 || tb + 31 > S.p_min - S.window)) {
+      bf16x8 pf[QT][NP];
+      S.weigh([&](int u, int c) { return L.key[b][u * (D / 32) + c][lane]; }, tb, ok, j, pf);
+#pragma unroll
+      for (int c = 0; c < VC; ++c) S.add_channel(c, L.value[b][c][lane], pf);
+      if (__builtin_amdgcn_readfirstlane(L.any_nan[b])) {
+        const uint32_t nan[2] = {L.nan[b][0][lane], L.nan[b][1][lane]};
+        S.spread_nan(nan, tb, ok, j);
+      }
+    }
+    ok = next;
+    __syncthreads();
+  }
+  if (!have) return;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const float L = row_sum(S.l[t]), inv = inverse(L);
-    const int32_t r = r0 + 16 * t + n;
+    const float total = row_sum(S.l[t]), inv = inverse(total);
+    const int32_t r = (w.tile * 4 + wave) * 16 * QT + 16 * t + n;
     if (r >= w.R) continue;
     const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
     const int32_t hq = w.h * w.G + r % w.G;
@@ -852,22 +1082,29 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows
       for (int c = 0; c < VC; ++c) x[c] = S.o[t][c][i] * inv;
       store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + (4 * j + i) * (D / 16), x);
     }
-    if (A.lse && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(S.m[t], L);
+    if (A.lse && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(S.m[t], total);
   }
 }
 
-// Joins the parts of a row's key range: a workgroup per (new token, query head),
-// whose wavefronts take every fourth part.
+// Joins the parts of a row's key range: a workgroup per row of the few-row
+// kernel's jobs.  A group of D/4 lanes takes a part, 16 B a lane, all parts' loads
+// on their way at a time.
 template <int D, typename T>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
-  constexpr int N = D / 64;
-  const int64_t row = blockIdx.x / A.kv.q_heads;
-  if (row < A.kv.starts[0] || row >= A.kv.starts[A.kv.n_seqs]) return;  // padding
-  const int lane = threadIdx.x & 63, wave = wave_index();
-  const int32_t hq = blockIdx.x % A.kv.q_heads;
-  const int64_t at = blockIdx.x;
-  const float* parts = A.part + at * A.splits * D;
-  const float* sums = A.part + static_cast<int64_t>(A.kv.n_rows) * A.kv.q_heads * A.splits * D + at * A.splits * 2;
+  constexpr int L = D / 4, groups = 256 / L;
+  const uint32_t job = blockIdx.x / A.part_rows;
+  const Job w = few_job(A, job);
+  const int32_t r = w.tile * 16 + static_cast<int32_t>(blockIdx.x % A.part_rows);
+  if (r >= w.R) return;
+  const int lane = threadIdx.x & 63, g = threadIdx.x / L, c = threadIdx.x % L;
+  const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
+  const int32_t hq = w.h * w.G + r % w.G;
+  const float* parts = A.part + static_cast<int64_t>(blockIdx.x) * A.splits * D;
+  const float* sums = A.part + A.part_sums + static_cast<int64_t>(blockIdx.x) * A.splits * 2;
+  f32x4 p[kMostSplits / groups];
+#pragma unroll
+  for (int k = 0; k < kMostSplits / groups; ++k)
+    p[k] = g + k * groups < A.splits ? *reinterpret_cast<const f32x4*>(parts + (g + k * groups) * D + 4 * c) : f32x4{0, 0, 0, 0};
   // lane i: the sums of parts i and 64 + i
   float m[2], l[2], M = -__builtin_inff();
 #pragma unroll
@@ -880,32 +1117,32 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) M = fmaxf(M, __shfl_xor(M, d));
   const float base = M == -__builtin_inff() ? 0.0f : M;
-  float L = 0.0f;
+  float total = 0.0f;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     m[k] = __builtin_amdgcn_exp2f(m[k] - base);
-    L += m[k] * l[k];
+    total += m[k] * l[k];
   }
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) L += __shfl_xor(L, d);
-  float x[N];
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
+  f32x4 x{0, 0, 0, 0};
 #pragma unroll
-  for (int c = 0; c < N; ++c) x[c] = 0.0f;
-#pragma unroll 4
-  for (int32_t k = wave; k < A.splits; k += 4) {
-    const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(k < 64 ? m[0] : m[1]), k & 63));
-#pragma unroll
-    for (int c = 0; c < N; ++c) x[c] += f * parts[k * D + c * 64 + lane];
+  for (int k = 0; k < kMostSplits / groups; ++k) {
+    const int at = g + k * groups;
+    const float f = __shfl(at < 64 ? m[0] : m[1], at & 63);  // parts that do not exist have 0
+    x += f * p[k];
   }
-  __shared__ float joined[4][D];
-#pragma unroll
-  for (int c = 0; c < N; ++c) joined[wave][c * 64 + lane] = x[c];
+  __shared__ f32x4 joined[256];
+  joined[threadIdx.x] = x;
   __syncthreads();
-  const float inv = inverse(L);
-  T* dst = static_cast<T*>(A.out) + row * A.out_stride + hq * D;
-  for (int c = threadIdx.x; c < D; c += 256)
-    dst[c] = static_cast<T>((joined[0][c] + joined[1][c] + joined[2][c] + joined[3][c]) * inv);
-  if (A.lse && threadIdx.x == 0) A.lse[at] = lse_of(base, L);
+  const float inv = inverse(total);
+  if (threadIdx.x < L) {
+#pragma unroll
+    for (int k = 1; k < groups; ++k) x += joined[k * L + threadIdx.x];
+    const float y[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    store_channels<4>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + 4 * threadIdx.x, y);
+  }
+  if (A.lse && threadIdx.x == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(base, total);
 }
 
 int64_t units(const KvArgs& A) { return A.max_new == 1 ? A.n_seqs : A.n_rows / 4 + 2ll * A.n_seqs; }
@@ -926,15 +1163,17 @@ hipError_t read(const ReadArgs& A, hipStream_t st) {
 
 template <int D, typename T>
 hipError_t attend(const AttendArgs& A, hipStream_t st) {
-  const int64_t blocks = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads * A.splits;
-  if (A.by_rows) {
+  if (A.units) {
+    const int64_t blocks = A.units * A.kv.kv_heads;
     k_attend_rows<D, T, row_tiles(D, Pieces<T>::n)><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !A.few) return e;
   }
-  k_attend<D, T><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
-  hipError_t e = hipGetLastError();
+  const int64_t jobs = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads;
+  k_attend<D, T><<<dim3(static_cast<unsigned>(jobs * A.splits)), 256, 0, st>>>(A);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.splits == 1) return e;
-  k_attend_join<D, T><<<dim3(static_cast<unsigned>(A.kv.n_rows * A.kv.q_heads)), 256, 0, st>>>(A);
+  k_attend_join<D, T><<<dim3(static_cast<unsigned>(jobs * A.part_rows)), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
@@ -953,24 +1192,35 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(read); }
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(attend); }
 
-// How a call is cut up.  Few query rows a sequence and KV head: tiles of 16 rows,
-// and parts of the key range so that about eight workgroups a CU exist, each with
-// 16 tiles of keys at least.  Many: a workgroup takes its wavefronts' rows.
+// How a call is cut up.  Sequences with at most kFewRows query rows a KV head:
+// tiles of 16 rows, and parts of the key range so that about eight workgroups a CU
+// exist, each with 16 tiles of keys at least.  The others: a workgroup takes the
+// rows of its four wavefronts, and the workgroups are numbered as append's units
+// are, so that a ragged batch has no more than one idle one a sequence and head.  A
+// batch that may hold both gets both kernels, each of which leaves the other's
+// sequences alone.
 AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
-  AttendPlan p;
-  const int64_t rows = static_cast<int64_t>(kv.max_new) * (kv.q_heads / kv.kv_heads);
-  const int64_t per = 4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3);
-  p.by_rows = rows > 64;
-  p.tiles = static_cast<int32_t>(p.by_rows ? (rows + per - 1) / per : (rows + 15) / 16);
+  AttendPlan p{};
+  const int64_t G = kv.q_heads / kv.kv_heads, rows = kv.max_new * G;
   p.splits = 1;
-  p.part_floats = 0;
-  if (p.by_rows) return p;
-  const int64_t blocks = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;
+  if (rows > kFewRows) {
+    const int64_t per = 4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3);
+    p.units = kv.n_rows * G / per + kv.n_seqs;
+    if (kv.n_seqs == 1) return p;
+  }
+  p.few = true;
+  const int64_t most = rows < kFewRows ? rows : kFewRows;
+  p.tiles = static_cast<int32_t>((most + 15) / 16);
+  p.part_rows = static_cast<int32_t>(most < 16 ? most : 16);
+  const int64_t jobs = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;
   const int64_t tokens = static_cast<int64_t>(kv.max_pages) << kv.page_shift;
-  int64_t s = blocks > 0 ? (2048 + blocks - 1) / blocks : 1;
+  int64_t s = (2048 + jobs - 1) / jobs;
   s = s < tokens / 512 ? s : tokens / 512;
-  p.splits = static_cast<int32_t>(s < 1 ? 1 : s > 128 ? 128 : s);
-  if (p.splits > 1) p.part_floats = static_cast<int64_t>(kv.n_rows) * kv.q_heads * p.splits * (head_dim + 2);
+  p.splits = static_cast<int32_t>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
+  if (p.splits > 1) {
+    p.part_sums = jobs * p.part_rows * p.splits * head_dim;
+    p.part_floats = p.part_sums + jobs * p.part_rows * p.splits * 2;
+  }
   return p;
 }
 

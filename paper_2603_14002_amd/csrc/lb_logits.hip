@@ -275,17 +275,18 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
   __shared__ float zt;
-  const int64_t row = blockIdx.x / A.splits;
+  const int64_t row = A.row0 + blockIdx.x / A.splits;
+  const int32_t part = static_cast<int32_t>(blockIdx.x % A.splits);
   Part<T> P;
   if (threadIdx.x == 0) zt = -__builtin_inff();
-  P.start(A, row, blockIdx.x % A.splits, A.splits, slots, shared);
+  P.start(A, row, part, A.splits, slots, shared);
   const int32_t target = A.score ? A.target[row] : -1;
   if (!P.sparse) __syncthreads();  // zt
   Sum s = block_sum(P.sum(target, &zt));  // its barrier also shows zt to all
   if (A.splits > 1) {
     if (threadIdx.x == 0) {
-      A.part[2 * static_cast<int64_t>(blockIdx.x)] = s.m;
-      A.part[2 * static_cast<int64_t>(blockIdx.x) + 1] = s.l;
+      A.part[2 * (row * A.splits + part)] = s.m;
+      A.part[2 * (row * A.splits + part) + 1] = s.l;
       if (target >= P.lo && target < P.hi) A.part[2 * A.rows * A.splits + row] = zt;
     }
     return;
@@ -300,8 +301,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void k_logits_join(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
   const int32_t parts = A.logprobs ? A.splits : 1;
-  const int64_t row = blockIdx.x / parts;
-  const int32_t part = blockIdx.x % parts;
+  const int64_t row = A.row0 + blockIdx.x / parts;
+  const int32_t part = static_cast<int32_t>(blockIdx.x % parts);
   Sum s{-__builtin_inff(), 0.0f};
   for (int32_t k = threadIdx.x; k < A.splits; k += 256) join(s, A.part[2 * (row * A.splits + k)], A.part[2 * (row * A.splits + k) + 1]);
   s = block_sum(s);
@@ -440,11 +441,19 @@ hipError_t run(const LogitArgs& A, hipStream_t st) {
     }
   const size_t per = (C + A.splits - 1) / A.splits + 8;
   const size_t lds = slots || A.r.mask ? ((per + 127) / 128 + 1) * 16 + slots * sizeof(Slot) : 0;
-  k_logits<T><<<dim3(static_cast<unsigned>(A.rows * A.splits)), 256, lds, st>>>(A, slots);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || A.splits == 1) return e;
-  k_logits_join<T><<<dim3(static_cast<unsigned>(A.logprobs ? A.rows * A.splits : A.rows)), 256, A.logprobs ? lds : 0, st>>>(A, slots);
-  return hipGetLastError();
+  // a launch has fewer than 2^32 threads
+  const int64_t most = (int64_t{1} << 23) / A.splits;
+  for (LogitArgs B = A; B.row0 < A.rows; B.row0 += most) {
+    const int64_t rows = A.rows - B.row0 < most ? A.rows - B.row0 : most;
+    k_logits<T><<<dim3(static_cast<unsigned>(rows * A.splits)), 256, lds, st>>>(B, slots);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (A.splits == 1) continue;
+    k_logits_join<T><<<dim3(static_cast<unsigned>(A.logprobs ? rows * A.splits : rows)), 256, A.logprobs ? lds : 0, st>>>(B, slots);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

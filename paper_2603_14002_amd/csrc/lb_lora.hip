@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
 constexpr int kUpChannels = 256;  // channels of d_out a workgroup takes: 64 a wavefront
 
 // h of a row as matrix operands.  In 16 bits it goes as its rounding and what that
-// leaves (2^-17 of it for bf16, 2^-22 for fp16): two products with the same
+// leaves (2^-16 of it for bf16, 2^-22 for fp16): two products with the same
 // weights, or, up to rank 16, side by side along the summed axis of one product.
 // fp16 is taken relative to the row's largest power of two, so that no h is out of
 // its range.

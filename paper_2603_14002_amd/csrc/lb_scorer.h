@@ -46,8 +46,10 @@ struct AttendArgs {
   float* part;  // partial sums of split key ranges (see lb_kv.hip)
   float scale2;  // scale * log2(e)
   int32_t window;
-  int32_t tiles, splits;
-  bool by_rows;
+  // the plan's
+  int32_t tiles, splits, part_rows;
+  int64_t units, part_sums;
+  bool few;
 };
 
 struct LoraArgs {
@@ -67,16 +69,19 @@ struct LogitArgs {
   int64_t out_stride;
   const int32_t* target;
   float *score, *lse, *part;
-  int64_t rows;
+  int64_t rows, row0;  // row0: the launch's first row
   int32_t classes, splits;
   lb_logit_rules r;
 };
 
-// the plan of an attention call: q rows a tile, and the parts a key range is cut into
+// How an attention call is cut up (see attend_plan).  Few-row kernel: `few`, tiles
+// of 16 query rows a sequence and KV head, the parts that a key range is cut into,
+// the rows of a tile whose parts are kept, the floats of these and where the parts'
+// sums start among them.  Many-row kernel: its units of rows, 0: none.
 struct AttendPlan {
-  int32_t tiles, splits;
-  bool by_rows;  // many query rows: wavefronts take rows, else parts of the keys
-  int64_t part_floats;
+  bool few;
+  int32_t tiles, splits, part_rows;
+  int64_t part_floats, part_sums, units;
 };
 AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype);  // part_floats is the same for every type
 

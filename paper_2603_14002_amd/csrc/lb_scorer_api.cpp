@@ -2,6 +2,7 @@
 // the device reads (page tables, lengths, ids) is checked by the kernels.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <exception>
@@ -51,6 +52,10 @@ lb_status entry(F&& body) noexcept {
 }
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// a launch has fewer than 2^32 threads: workgroups of 256 threads that a call may need
+constexpr int64_t kMostGroups = (1 << 24) - 1;
+constexpr float kLog2e = 1.4426950408889634f;
+
 int64_t size_of(int32_t dtype) { return dtype == LB_F32 ? 4 : 2; }
 
 void check_dtype(int32_t dtype) {
@@ -74,7 +79,7 @@ KvArgs kv_args(const lb_kv_cache* c, const lb_kv_batch* b, int32_t q_heads) {
   need(aligned(c->pages), "pages must be 16-B aligned");
   need((reinterpret_cast<uintptr_t>(c->flags) & 3) == 0, "flags must be 4-B aligned");
   need(b->n_seqs >= 0 && b->n_rows >= 0, "n_seqs and n_rows must not be negative");
-  need(b->n_seqs <= (1 << 24) && b->n_rows <= (1 << 28), "n_seqs at most 2^24, n_rows at most 2^28");
+  need(b->n_seqs <= (1 << 22) && b->n_rows <= (1 << 24), "n_seqs at most 2^22, n_rows at most 2^24");
   KvArgs a{};
   a.q_heads = q_heads;
   a.kv_heads = c->kv_heads;
@@ -215,16 +220,15 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     AttendArgs A{};
     A.kv = kv_args(cache, batch, q_heads);
     check_heads(A.kv);
-    need(std::isfinite(scale), "scale must be finite");
+    need(std::isfinite(scale * kLog2e), "scale must be finite");
     need(window >= 0, "window must not be negative");
     const int64_t width = static_cast<int64_t>(q_heads) * cache->head_dim, rows = A.kv.n_rows;
     check_rows(q, q_stride, width, dtype, rows, "null device pointer: q", "q must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     check_rows(out, out_stride, width, dtype, rows, "null device pointer: out", "out must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     if (rows == 0) return hipSuccess;
     const AttendPlan p = attend_plan(A.kv, cache->head_dim, dtype);
-    need(static_cast<int64_t>(A.kv.n_seqs) * p.tiles * A.kv.kv_heads * p.splits <= 0x7FFFFFFF,
-         "too much work for one call: n_seqs * max_new * q_heads is too large");
-    need(p.splits == 1 || rows * q_heads <= 0x7FFFFFFF, "too much work for one call: n_rows * q_heads is too large");
+    need(static_cast<int64_t>(A.kv.n_seqs) * p.tiles * A.kv.kv_heads * p.splits <= kMostGroups && p.units * A.kv.kv_heads <= kMostGroups,
+         "too much work for one call: n_seqs or n_rows * q_heads is too large");
     need(p.part_floats == 0 || (workspace && aligned(workspace) && workspace_bytes >= p.part_floats * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_kv_attend_workspace says");
     A.q = q;
@@ -233,11 +237,14 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     A.out_stride = out_stride;
     A.lse = lse;
     A.part = static_cast<float*>(workspace);
-    A.scale2 = scale * 1.4426950408889634f;
-    A.window = window;
+    A.scale2 = scale * kLog2e;
+    A.window = window < (1 << 30) ? window : 0;  // a sequence has at most 2^30 tokens
     A.tiles = p.tiles;
     A.splits = p.splits;
-    A.by_rows = p.by_rows;
+    A.part_rows = p.part_rows;
+    A.units = p.units;
+    A.part_sums = p.part_sums;
+    A.few = p.few;
     return launch_kv_attend(A, cache->head_dim, dtype, static_cast<hipStream_t>(stream));
   });
 }
@@ -271,7 +278,7 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     need(aligned(a) && aligned(b), "a and b must be 16-B aligned");
     need(adapter || rows == 0, "null device pointer: adapter");
     if (rows == 0) return hipSuccess;
-    need(((rows + 15) / 16) * ((d_out + 255) / 256) <= (1 << 24), "too much work for one call: rows * d_out is too large");
+    need(((rows + 15) / 16) * ((d_out + 255) / 256) <= kMostGroups, "too much work for one call: rows * d_out is too large");
     LoraArgs A{};
     need(workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4,
          "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says");
@@ -323,8 +330,9 @@ lb_status lb_logits_adjust(int32_t dtype, int64_t rows, int32_t classes, const v
     A.r.temperature = A.r.repetition = 1.0f;
     if (rules) {
       A.r = *rules;
-      need(std::isfinite(A.r.temperature) && A.r.temperature > 0, "temperature must be positive and finite");
-      need(std::isfinite(A.r.repetition) && A.r.repetition > 0, "repetition must be positive and finite");
+      // their reciprocals have to be numbers too
+      need(std::isfinite(A.r.temperature) && A.r.temperature >= FLT_MIN, "temperature must be a normal number above 0");
+      need(std::isfinite(A.r.repetition) && A.r.repetition >= FLT_MIN, "repetition must be a normal number above 0");
       need(std::isfinite(A.r.presence) && std::isfinite(A.r.frequency), "presence and frequency must be finite");
       need(A.r.history_width >= 0 && A.r.bias_width >= 0 && A.r.mask_rows >= 0, "widths must not be negative");
       if (!A.r.history) A.r.history_width = 0;
@@ -337,7 +345,6 @@ lb_status lb_logits_adjust(int32_t dtype, int64_t rows, int32_t classes, const v
     }
     if (rows == 0) return hipSuccess;
     A.splits = logits_splits(rows, classes);
-    need(rows * A.splits <= 0x7FFFFFFF, "too many rows for one call");
     need(A.splits == 1 || (workspace && aligned(workspace) && workspace_bytes >= (rows * A.splits * 2 + rows) * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_logits_workspace says");
     A.logits = logits;

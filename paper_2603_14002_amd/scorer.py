@@ -10,7 +10,6 @@ current stream of the tensors' device).  Every step runs in the library's HIP ke
 from __future__ import annotations
 
 import ctypes
-import functools
 from typing import Optional
 
 LB_F32, LB_BF16, LB_F16 = 0, 1, 2
@@ -64,76 +63,86 @@ def declare(L) -> None:
         f.argtypes = at[name]
 
 
-def _binding():
+# torch, this package, torch's current raw stream of a device and its current device, set by _load() before
+# the first use: the package can be imported without torch, and a call of a few microseconds has no time for
+# an import statement in each helper
+torch = _lbm = _raw_stream = _current_device = None
+_DTYPE = {}
+
+
+def _load() -> None:
+    global torch, _lbm, _raw_stream, _current_device
+    if torch is not None:
+        return
+    import torch as t
     import paper_2603_14002_amd as lbm
-    return lbm
-
-
-@functools.lru_cache(maxsize=None)
-def _dtypes():
-    import torch
-    return {torch.float32: LB_F32, torch.bfloat16: LB_BF16, torch.float16: LB_F16}
+    _DTYPE.update({t.float32: LB_F32, t.bfloat16: LB_BF16, t.float16: LB_F16})
+    _lbm, _current_device = lbm, t.cuda.current_device
+    # what torch.cuda.current_stream(i).cuda_stream reads, without making a Stream object (2.8 us)
+    _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
+    torch = t
 
 
 def _bad(msg: str):
-    lbm = _binding()
-    raise lbm.LBError(lbm.LB_ERR_INVALID_ARG, msg)
+    _load()
+    raise _lbm.LBError(_lbm.LB_ERR_INVALID_ARG, msg)
 
 
 def _dtype(t, name: str) -> int:
-    d = _dtypes().get(t.dtype)
+    if torch is None:
+        _load()
+    d = _DTYPE.get(t.dtype)
     if d is None:
         _bad(f"{name} must be float32, bfloat16 or float16")
     return d
 
 
-def _call(dev, stream, name: str, *args) -> None:
+def _call(g: int, stream, name: str, *args) -> None:
     """Calls an entry point with `stream` last, on the tensors' device."""
-    import torch
-    lbm = _binding()
-    if dev.type != "cuda":
+    if g < 0:
         _bad(f"{name}: the tensors must be on a GPU")
-    f = getattr(lbm.lib(), name)
-    here = torch.cuda.current_device()
-    if dev.index is None or dev.index == here:
-        st = f(*args, lbm._stream_ptr(stream))
+    f = getattr(_lbm._lib or _lbm.lib(), name)
+    if g == _current_device():
+        st = f(*args, _raw_stream(g) if stream is None else _lbm._stream_ptr(stream))
     else:
-        with torch.cuda.device(dev):
-            st = f(*args, lbm._stream_ptr(stream))
-    if st != lbm.LB_OK:
-        raise lbm.LBError(st, lbm.lb_last_error())
+        with torch.cuda.device(g):
+            st = f(*args, _raw_stream(g) if stream is None else _lbm._stream_ptr(stream))
+    if st:
+        raise _lbm.LBError(st, _lbm.lb_last_error())
 
 
-def _same_device(dev, **tensors) -> None:
+def _elsewhere(g: int, **tensors) -> None:
+    """Refuses the call for the first of its tensors that is not on device `g` (-1: not on a GPU)."""
     for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            _bad(f"{name} is on {t.device}, the call's other tensors are on {dev}")
+        if t is not None and t.get_device() != g:
+            _bad(f"{name} is on {t.device}, the call's other tensors are on {f'cuda:{g}' if g >= 0 else 'cpu'}")
 
 
-def _scratch(dev, stream, nbytes: int, given, name: str):
-    """The workspace given, or a new one that lives until the stream is done with it."""
-    import torch
+def _empty(shape, dtype, like, stream):
+    """A new tensor on `like`'s device for a call on `stream`.  For another stream than torch's current one it
+    comes from that stream's own pool (a block of the current stream's pool may still be in use by work queued
+    there), and it is also kept for work that the current stream has been given when it is dropped."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.device(like.device):
+        here = torch.cuda.current_stream()
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+            t = torch.empty(shape, dtype=dtype, device=like.device)
+        t.record_stream(here)
+    return t
+
+
+def _scratch(like, stream, nbytes: int, given, name: str):
+    """The workspace given, or a new one: its address (None: none is needed), its size and the tensor itself,
+    which has to live until the call has been enqueued."""
     if given is not None:
-        if given.device != dev or not given.is_contiguous():
-            _bad(f"{name}: the workspace must be contiguous, on {dev}")
-        return given, given.numel() * given.element_size()
+        if given.get_device() != like.get_device() or not given.is_contiguous():
+            _bad(f"{name}: the workspace must be contiguous, on {like.device}")
+        return given.data_ptr(), given.numel() * given.element_size(), given
     if nbytes == 0:
-        return None, 0
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    if stream is not None:
-        with torch.cuda.device(dev):
-            ws.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-    return ws, nbytes
-
-
-def _empty(like, stream, shape, dtype=None):
-    """A new output, safe to drop while `stream` still writes it."""
-    import torch
-    out = torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-    if stream is not None:
-        with torch.cuda.device(like.device):
-            out.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-    return out
+        return None, 0, None
+    ws = _empty(nbytes, torch.uint8, like, stream)
+    return ws.data_ptr(), nbytes, ws
 
 
 def _ptr(t) -> Optional[int]:
@@ -142,33 +151,40 @@ def _ptr(t) -> Optional[int]:
 
 def _ints(t, name: str, shape) -> None:
     """A contiguous int32 tensor; None in `shape`: any size there."""
-    import torch
-    if t.dtype != torch.int32 or not t.is_contiguous():
+    if t.dtype is not torch.int32 or not t.is_contiguous():
         _bad(f"{name} must be a contiguous int32 tensor")
-    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        _bad(f"{name} has shape {tuple(t.shape)}, expected {tuple('any' if n is None else n for n in shape)}")
+    at = t.shape
+    if len(at) != len(shape):
+        _bad(f"{name} has shape {tuple(at)}, expected {tuple('any' if n is None else n for n in shape)}")
+    for n, m in zip(shape, at):
+        if n is not None and n != m:
+            _bad(f"{name} has shape {tuple(at)}, expected {tuple('any' if n is None else n for n in shape)}")
 
 
 def _heads(t, name: str, rows: int, heads: Optional[int], dim: int, dtype) -> int:
     """Row stride of [rows, heads, dim] whose heads and channels lie together."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _bad(f"{name} is {t.dtype}, expected {dtype}")
-    if t.dim() != 3 or t.shape[0] != rows or t.shape[2] != dim or (heads is not None and t.shape[1] != heads):
-        _bad(f"{name} has shape {tuple(t.shape)}, expected ({rows}, {'heads' if heads is None else heads}, {dim})")
-    if rows and ((t.shape[1] > 1 and t.stride(1) != dim) or t.stride(2) != 1):
+    at = t.shape
+    if len(at) != 3 or at[0] != rows or at[2] != dim or (heads is not None and at[1] != heads):
+        _bad(f"{name} has shape {tuple(at)}, expected ({rows}, {'heads' if heads is None else heads}, {dim})")
+    s0, s1, s2 = t.stride()
+    if rows and ((at[1] > 1 and s1 != dim) or s2 != 1):
         _bad(f"{name}: the heads of a row must lie one after the other")
-    return t.stride(0) if rows > 1 else t.shape[1] * dim
+    return s0 if rows > 1 else at[1] * dim
 
 
 def _rows(t, name: str, rows: int, width: int, dtype) -> int:
     """Row stride of [rows, width] whose rows are contiguous."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         _bad(f"{name} is {t.dtype}, expected {dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
-        _bad(f"{name} has shape {tuple(t.shape)}, expected ({rows}, {width})")
-    if width > 1 and rows and t.stride(1) != 1:
+    at = t.shape
+    if len(at) != 2 or at[0] != rows or at[1] != width:
+        _bad(f"{name} has shape {tuple(at)}, expected ({rows}, {width})")
+    s0, s1 = t.stride()
+    if width > 1 and rows and s1 != 1:
         _bad(f"{name}: the values of a row must lie one after the other")
-    return t.stride(0) if rows > 1 else width
+    return s0 if rows > 1 else width
 
 
 # ------------------------------------------------------------------ descriptors
@@ -179,19 +195,22 @@ class KVCache:
     [n_pages, kv_heads, page_tokens * (head_dim + head_dim / 16)], `flags` None or an int32
     tensor of one element that faults of the data are or-ed into."""
 
-    __slots__ = ("pages", "flags", "page_tokens", "kv_heads", "head_dim", "desc", "ref")
+    __slots__ = ("pages", "flags", "page_tokens", "kv_heads", "head_dim", "device", "desc", "ref")
 
     def __init__(self, pages, page_tokens: int, kv_heads: int, head_dim: int, flags=None):
-        import torch
-        if pages.dtype != torch.uint8 or not pages.is_contiguous():
+        if torch is None:
+            _load()
+        if pages.dtype is not torch.uint8 or not pages.is_contiguous():
             _bad("pages must be a contiguous uint8 tensor")
-        if pages.dim() != 3 or pages.shape[1] != kv_heads or pages.shape[2] != self.page_bytes(page_tokens, 1, head_dim):
-            _bad(f"pages has shape {tuple(pages.shape)}, expected (pages, {kv_heads}, {self.page_bytes(page_tokens, 1, head_dim)})")
-        if flags is not None and (flags.dtype != torch.int32 or flags.numel() != 1 or flags.device != pages.device):
+        at = pages.shape
+        if len(at) != 3 or at[1] != kv_heads or at[2] != page_tokens * (head_dim + head_dim // 16):
+            _bad(f"pages has shape {tuple(at)}, expected (pages, {kv_heads}, {self.page_bytes(page_tokens, 1, head_dim)})")
+        self.device = pages.get_device()
+        if flags is not None and (flags.dtype is not torch.int32 or flags.numel() != 1 or flags.get_device() != self.device):
             _bad("flags must be one int32 on the pages' device")
         self.pages, self.flags = pages, flags
         self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
-        self.desc = lb_kv_cache(pages.data_ptr(), pages.shape[0], page_tokens, kv_heads, head_dim, 0, _ptr(flags))
+        self.desc = lb_kv_cache(pages.data_ptr(), at[0], page_tokens, kv_heads, head_dim, 0, _ptr(flags))
         self.ref = ctypes.addressof(self.desc)
 
     @staticmethod
@@ -201,7 +220,7 @@ class KVCache:
     @classmethod
     def empty(cls, n_pages: int, page_tokens: int, kv_heads: int, head_dim: int, device="cuda"):
         """A cache in new memory, with a flags word."""
-        import torch
+        _load()
         pages = torch.empty((n_pages, kv_heads, cls.page_bytes(page_tokens, 1, head_dim)), dtype=torch.uint8, device=device)
         return cls(pages, page_tokens, kv_heads, head_dim, torch.zeros(1, dtype=torch.int32, device=device))
 
@@ -215,14 +234,18 @@ class KVBatch:
     [n_seqs] and pages [n_seqs, max_pages]; `n_rows` rows of activations, at most `max_new`
     new tokens a sequence.  The tensors may be changed between calls."""
 
-    __slots__ = ("starts", "lengths", "pages", "n_rows", "desc", "ref")
+    __slots__ = ("starts", "lengths", "pages", "n_rows", "device", "desc", "ref")
 
     def __init__(self, starts, lengths, pages, n_rows: int, max_new: int):
+        if torch is None:
+            _load()
         n = lengths.shape[0] if lengths.dim() else 0
         _ints(starts, "starts", (n + 1,))
         _ints(lengths, "lengths", (n,))
         _ints(pages, "the page table", (n, None))
-        _same_device(starts.device, lengths=lengths, pages=pages)
+        self.device = starts.get_device()
+        if lengths.get_device() != self.device or pages.get_device() != self.device:
+            _elsewhere(self.device, lengths=lengths, pages=pages)
         self.starts, self.lengths, self.pages, self.n_rows = starts, lengths, pages, n_rows
         self.desc = lb_kv_batch(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), n, n_rows, pages.shape[1], max_new)
         self.ref = ctypes.addressof(self.desc)
@@ -231,14 +254,15 @@ class KVBatch:
 class Rope:
     """Angles of the rotation (``lb_rope``): cos and sin, float32 [positions, rot_dim / 2]."""
 
-    __slots__ = ("cos", "sin", "desc", "ref")
+    __slots__ = ("cos", "sin", "device", "desc", "ref")
 
     def __init__(self, cos, sin, layout: int = LB_ROPE_HALF):
-        import torch
-        if cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.dim() != 2 or cos.shape != sin.shape \
+        if torch is None:
+            _load()
+        if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or cos.dim() != 2 or cos.shape != sin.shape \
                 or not cos.is_contiguous() or not sin.is_contiguous() or cos.device != sin.device:
             _bad("cos and sin must be contiguous float32 [positions, rot_dim / 2] on one device")
-        self.cos, self.sin = cos, sin
+        self.cos, self.sin, self.device = cos, sin, cos.get_device()
         self.desc = lb_rope(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], layout, 0)
         self.ref = ctypes.addressof(self.desc)
 
@@ -252,26 +276,30 @@ class LogitRules:
 
     def __init__(self, temperature: float = 1.0, history=None, repetition: float = 1.0, presence: float = 0.0,
                  frequency: float = 0.0, bias_ids=None, bias_values=None, mask=None, mask_row=None):
-        import torch
+        if torch is None:
+            _load()
         self.history, self.bias_ids, self.bias_values, self.mask, self.mask_row = history, bias_ids, bias_values, mask, mask_row
+        h = bi = bv = mk = mr = None
+        hw = bw = per_row = masks = 0
         if history is not None:
             _ints(history, "history", (None, None))
+            h, hw = history.data_ptr(), history.shape[1]
         if (bias_ids is None) != (bias_values is None):
             _bad("bias_ids and bias_values belong together")
         if bias_ids is not None:
             _ints(bias_ids, "bias_ids", (None, None))
-            if bias_values.dtype != torch.float32 or bias_values.shape != bias_ids.shape or not bias_values.is_contiguous():
+            if bias_values.dtype is not torch.float32 or bias_values.shape != bias_ids.shape or not bias_values.is_contiguous():
                 _bad("bias_values must be contiguous float32 of bias_ids' shape")
+            bi, bv, bw, per_row = bias_ids.data_ptr(), bias_values.data_ptr(), bias_ids.shape[1], int(bias_ids.shape[0] != 1)
         if mask is not None:
             _ints(mask, "mask", (None, None))
+            mk, masks = mask.data_ptr(), mask.shape[0]
         if mask_row is not None:
             if mask is None:
                 _bad("mask_row needs a mask")
             _ints(mask_row, "mask_row", (None,))
-        self.desc = lb_logit_rules(temperature, repetition, presence, frequency, _ptr(history), _ptr(bias_ids),
-                                   _ptr(bias_values), _ptr(mask), _ptr(mask_row),
-                                   0 if history is None else history.shape[1], 0 if bias_ids is None else bias_ids.shape[1],
-                                   0, 0 if mask is None else mask.shape[0])
+            mr = mask_row.data_ptr()
+        self.desc = lb_logit_rules(temperature, repetition, presence, frequency, h, bi, bv, mk, mr, hw, bw, per_row, masks)
         self.ref = ctypes.addressof(self.desc)
 
 
@@ -281,12 +309,11 @@ class LogitRules:
 def lb_rope_table(positions: int, rot_dim: int, base: float = 10000.0, scaling: int = LB_ROPE_PLAIN, factor: float = 1.0,
                   trained: float = 0.0, low: float = 1.0, high: float = 4.0):
     """Host tables (cos, sin), float32 [positions, rot_dim / 2]."""
-    import torch
-    lbm = _binding()
+    _load()
     cos = torch.empty((max(positions, 0), max(rot_dim, 0) // 2), dtype=torch.float32)
     sin = torch.empty_like(cos)
-    lbm._check(lbm.lib().lb_rope_table(positions, rot_dim, base, scaling, factor, trained, low, high, cos.data_ptr(),
-                                       sin.data_ptr()))
+    _lbm._check(_lbm.lib().lb_rope_table(positions, rot_dim, base, scaling, factor, trained, low, high, cos.data_ptr(),
+                                         sin.data_ptr()))
     return cos, sin
 
 
@@ -294,19 +321,21 @@ def lb_kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope: Optional[Rope] =
     """Appends the batch's new keys and values ([n_rows, kv_heads, head_dim]) to the cache, rotated
     if `rope` is given; q [n_rows, q_heads, head_dim] or None.  Returns the rotated queries (q_out,
     which may be q itself, or a new tensor)."""
-    dt, n, H, D = _dtype(k, "k"), batch.n_rows, cache.kv_heads, cache.head_dim
-    dev = cache.pages.device
-    _same_device(dev, starts=batch.starts, k=k, v=v, q=q, q_out=q_out, cos=None if rope is None else rope.cos)
-    ks, vs = _heads(k, "k", n, H, D, k.dtype), _heads(v, "v", n, H, D, k.dtype)
+    dt, dtype, n, H, D, g = _dtype(k, "k"), k.dtype, batch.n_rows, cache.kv_heads, cache.head_dim, cache.device
+    ks, vs = _heads(k, "k", n, H, D, dtype), _heads(v, "v", n, H, D, dtype)
+    if batch.device != g or k.get_device() != g or v.get_device() != g or (rope is not None and rope.device != g):
+        _elsewhere(g, starts=batch.starts, k=k, v=v, cos=None if rope is None else rope.cos)
     hq = qs = os = 0
     if q is not None:
-        qs, hq = _heads(q, "q", n, None, D, k.dtype), q.shape[1]
+        qs, hq = _heads(q, "q", n, None, D, dtype), q.shape[1]
         if q_out is None:
-            q_out = _empty(q, stream, (n, hq, D))
-        os = _heads(q_out, "q_out", n, hq, D, k.dtype)
+            q_out = _empty((n, hq, D), dtype, q, stream)
+        os = _heads(q_out, "q_out", n, hq, D, dtype)
+        if q.get_device() != g or q_out.get_device() != g:
+            _elsewhere(g, q=q, q_out=q_out)
     elif q_out is not None:
         _bad("q_out needs q")
-    _call(dev, stream, "lb_kv_append", cache.ref, batch.ref, None if rope is None else rope.ref, dt, hq, _ptr(q), qs,
+    _call(g, stream, "lb_kv_append", cache.ref, batch.ref, None if rope is None else rope.ref, dt, hq, _ptr(q), qs,
           k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), os)
     return q_out
 
@@ -314,23 +343,22 @@ def lb_kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope: Optional[Rope] =
 def lb_kv_read(cache: KVCache, batch: KVBatch, dtype=None, k_out=None, v_out=None, stream=None):
     """The keys and values that the cache holds of the batch's new tokens, [n_rows, kv_heads, head_dim] each
     (k_out and v_out, or new tensors of `dtype`, float32 if None; of rows that are padding nothing is written)."""
-    import torch
-    n, H, D, dev = batch.n_rows, cache.kv_heads, cache.head_dim, cache.pages.device
+    n, H, D, g = batch.n_rows, cache.kv_heads, cache.head_dim, cache.device
     if dtype is None:
         given = k_out if k_out is not None else v_out
         dtype = torch.float32 if given is None else given.dtype
-    k_out = _empty(cache.pages, stream, (n, H, D), dtype) if k_out is None else k_out
-    v_out = _empty(cache.pages, stream, (n, H, D), dtype) if v_out is None else v_out
-    _same_device(dev, starts=batch.starts, k_out=k_out, v_out=v_out)
+    k_out = _empty((n, H, D), dtype, cache.pages, stream) if k_out is None else k_out
+    v_out = _empty((n, H, D), dtype, cache.pages, stream) if v_out is None else v_out
     ks, vs = _heads(k_out, "k_out", n, H, D, dtype), _heads(v_out, "v_out", n, H, D, dtype)
-    _call(dev, stream, "lb_kv_read", cache.ref, batch.ref, _dtype(k_out, "k_out"), k_out.data_ptr(), ks, v_out.data_ptr(), vs)
+    if batch.device != g or k_out.get_device() != g or v_out.get_device() != g:
+        _elsewhere(g, starts=batch.starts, k_out=k_out, v_out=v_out)
+    _call(g, stream, "lb_kv_read", cache.ref, batch.ref, _dtype(k_out, "k_out"), k_out.data_ptr(), ks, v_out.data_ptr(), vs)
     return k_out, v_out
 
 
 def lb_kv_attend_workspace(cache: KVCache, batch: KVBatch, q_heads: int) -> int:
-    lbm = _binding()
-    need = ctypes.c_int64()
-    lbm._check(lbm.lib().lb_kv_attend_workspace(cache.ref, batch.ref, q_heads, ctypes.addressof(need)))
+    need = _L()
+    _lbm._check((_lbm._lib or _lbm.lib()).lb_kv_attend_workspace(cache.ref, batch.ref, q_heads, ctypes.addressof(need)))
     return need.value
 
 
@@ -338,28 +366,28 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
                  workspace=None, stream=None):
     """Attention of the batch's new tokens, q [n_rows, q_heads, head_dim].  Returns (out, lse): out (or a
     new tensor) as q, lse float32 [n_rows, q_heads] or None."""
-    import torch
-    dt, n, D, dev = _dtype(q, "q"), batch.n_rows, cache.head_dim, cache.pages.device
-    qs = _heads(q, "q", n, None, D, q.dtype)
+    dt, dtype, n, D, g = _dtype(q, "q"), q.dtype, batch.n_rows, cache.head_dim, cache.device
+    qs = _heads(q, "q", n, None, D, dtype)
     hq = q.shape[1]
     if out is None:
-        out = _empty(q, stream, (n, hq, D))
-    os = _heads(out, "out", n, hq, D, q.dtype)
+        out = _empty((n, hq, D), dtype, q, stream)
+    os = _heads(out, "out", n, hq, D, dtype)
     if lse is None and want_lse:
-        lse = _empty(q, stream, (n, hq), torch.float32)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (n, hq) or not lse.is_contiguous()):
+        lse = _empty((n, hq), torch.float32, q, stream)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, hq) or not lse.is_contiguous()):
         _bad(f"lse must be contiguous float32 ({n}, {hq})")
-    _same_device(dev, starts=batch.starts, q=q, out=out, lse=lse)
-    ws, nbytes = _scratch(dev, stream, 0 if workspace is not None else lb_kv_attend_workspace(cache, batch, hq), workspace, "lb_kv_attend")
-    _call(dev, stream, "lb_kv_attend", cache.ref, batch.ref, dt, hq, q.data_ptr(), qs, scale, window, out.data_ptr(), os,
-          _ptr(lse), _ptr(ws), nbytes)
+    if batch.device != g or q.get_device() != g or out.get_device() != g or (lse is not None and lse.get_device() != g):
+        _elsewhere(g, starts=batch.starts, q=q, out=out, lse=lse)
+    ws, nbytes, _held = _scratch(q, stream, 0 if workspace is not None else lb_kv_attend_workspace(cache, batch, hq), workspace, "lb_kv_attend")
+    _call(g, stream, "lb_kv_attend", cache.ref, batch.ref, dt, hq, q.data_ptr(), qs, scale, window, out.data_ptr(), os,
+          _ptr(lse), ws, nbytes)
     return out, lse
 
 
 def lb_lora_workspace(rows: int, d_in: int, d_out: int, rank: int) -> int:
-    lbm = _binding()
-    need = ctypes.c_int64()
-    lbm._check(lbm.lib().lb_lora_workspace(rows, d_in, d_out, rank, ctypes.addressof(need)))
+    _load()
+    need = _L()
+    _lbm._check((_lbm._lib or _lbm.lib()).lb_lora_workspace(rows, d_in, d_out, rank, ctypes.addressof(need)))
     return need.value
 
 
@@ -367,31 +395,35 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     """y [rows, d_out] + scale[adapter] * b[adapter] (a[adapter] x), x [rows, d_in], a [n, rank, d_in],
     b [n, d_out, rank], adapter int32 [rows], scale float32 [n] or None.  Written to `out` (None: y itself),
     which is returned."""
-    import torch
-    dt, dev = _dtype(y, "y"), y.device
+    dt, dtype, g = _dtype(y, "y"), y.dtype, y.get_device()
     if x.dim() != 2 or y.dim() != 2 or a.dim() != 3 or b.dim() != 3:
         _bad("x and y must have 2 dimensions, a and b 3")
-    rows, d_in, d_out, (n, rank) = y.shape[0], x.shape[1], y.shape[1], a.shape[:2]
-    out = y if out is None else out
-    xs, ys, os = _rows(x, "x", rows, d_in, y.dtype), _rows(y, "y", rows, d_out, y.dtype), _rows(out, "out", rows, d_out, y.dtype)
-    if a.dtype != y.dtype or tuple(a.shape) != (n, rank, d_in) or not a.is_contiguous():
-        _bad(f"a must be contiguous {y.dtype} ({n}, {rank}, {d_in})")
-    if b.dtype != y.dtype or tuple(b.shape) != (n, d_out, rank) or not b.is_contiguous():
-        _bad(f"b must be contiguous {y.dtype} ({n}, {d_out}, {rank})")
+    (rows, d_out), d_in, (n, rank, _) = y.shape, x.shape[1], a.shape
+    xs, ys = _rows(x, "x", rows, d_in, dtype), _rows(y, "y", rows, d_out, dtype)
+    if out is None:
+        out, os = y, ys
+    else:
+        os = _rows(out, "out", rows, d_out, dtype)
+    if a.dtype is not dtype or a.shape != (n, rank, d_in) or not a.is_contiguous():
+        _bad(f"a must be contiguous {dtype} ({n}, {rank}, {d_in})")
+    if b.dtype is not dtype or b.shape != (n, d_out, rank) or not b.is_contiguous():
+        _bad(f"b must be contiguous {dtype} ({n}, {d_out}, {rank})")
     _ints(adapter, "adapter", (rows,))
-    if scale is not None and (scale.dtype != torch.float32 or tuple(scale.shape) != (n,) or not scale.is_contiguous()):
+    if scale is not None and (scale.dtype is not torch.float32 or scale.shape != (n,) or not scale.is_contiguous()):
         _bad(f"scale must be contiguous float32 ({n},)")
-    _same_device(dev, x=x, a=a, b=b, adapter=adapter, scale=scale, out=out)
-    ws, nbytes = _scratch(dev, stream, 0 if workspace is not None else lb_lora_workspace(rows, d_in, d_out, rank), workspace, "lb_lora_add")
-    _call(dev, stream, "lb_lora_add", dt, rows, d_in, d_out, rank, n, x.data_ptr(), xs, y.data_ptr(), ys, a.data_ptr(),
-          b.data_ptr(), adapter.data_ptr(), _ptr(scale), out.data_ptr(), os, _ptr(ws), nbytes)
+    if x.get_device() != g or a.get_device() != g or b.get_device() != g or adapter.get_device() != g or out.get_device() != g \
+            or (scale is not None and scale.get_device() != g):
+        _elsewhere(g, x=x, a=a, b=b, adapter=adapter, scale=scale, out=out)
+    ws, nbytes, _held = _scratch(y, stream, 0 if workspace is not None else lb_lora_workspace(rows, d_in, d_out, rank), workspace, "lb_lora_add")
+    _call(g, stream, "lb_lora_add", dt, rows, d_in, d_out, rank, n, x.data_ptr(), xs, y.data_ptr(), ys, a.data_ptr(),
+          b.data_ptr(), adapter.data_ptr(), _ptr(scale), out.data_ptr(), os, ws, nbytes)
     return out
 
 
 def lb_logits_workspace(rows: int, classes: int) -> int:
-    lbm = _binding()
-    need = ctypes.c_int64()
-    lbm._check(lbm.lib().lb_logits_workspace(rows, classes, ctypes.addressof(need)))
+    _load()
+    need = _L()
+    _lbm._check((_lbm._lib or _lbm.lib()).lb_logits_workspace(rows, classes, ctypes.addressof(need)))
     return need.value
 
 
@@ -400,39 +432,42 @@ def lb_logits_adjust(logits, rules: Optional[LogitRules] = None, target=None, wa
     """Adjusted log-probabilities of logits [rows, classes].  Returns (logprobs, score, lse): float32
     [rows, classes] (None unless wanted or given), float32 [rows] at target int32 [rows] (None without
     one), and float32 [rows]."""
-    import torch
-    dt, dev = _dtype(logits, "logits"), logits.device
+    dt, g = _dtype(logits, "logits"), logits.get_device()
     if logits.dim() != 2:
         _bad("logits must have 2 dimensions")
     rows, classes = logits.shape
     stride = _rows(logits, "logits", rows, classes, logits.dtype)
     os = classes
-    if logprobs is None and want_logprobs:
-        logprobs = _empty(logits, stream, (rows, classes), torch.float32)
     if logprobs is not None:
         os = _rows(logprobs, "logprobs", rows, classes, torch.float32)
+        if logprobs.get_device() != g:
+            _elsewhere(g, logprobs=logprobs)
+    elif want_logprobs:
+        logprobs = _empty((rows, classes), torch.float32, logits, stream)
     score = None
     if target is not None:
         _ints(target, "target", (rows,))
-        score = _empty(logits, stream, (rows,), torch.float32)
-    lse = _empty(logits, stream, (rows,), torch.float32)
+        if target.get_device() != g:
+            _elsewhere(g, target=target)
+        score = _empty(rows, torch.float32, logits, stream)
+    lse = _empty(rows, torch.float32, logits, stream)
     ref = None
     if rules is not None:
-        if rules.history is not None and rules.history.shape[0] != rows:
-            _bad(f"history has {rules.history.shape[0]} rows, the logits {rows}")
-        if rules.bias_ids is not None:
-            if rules.bias_ids.shape[0] not in (1, rows):
-                _bad(f"bias_ids has {rules.bias_ids.shape[0]} rows, the logits {rows}")
-            rules.desc.bias_per_row = int(rules.bias_ids.shape[0] != 1)
-        if rules.mask is not None and rules.mask.shape[1] != (classes + 31) // 32:
-            _bad(f"mask has {rules.mask.shape[1]} words a row, expected {(classes + 31) // 32}")
-        if rules.mask_row is not None and rules.mask_row.shape[0] != rows:
-            _bad(f"mask_row has {rules.mask_row.shape[0]} entries, expected {rows}")
-        _same_device(dev, history=rules.history, bias_ids=rules.bias_ids, bias_values=rules.bias_values, mask=rules.mask,
-                     mask_row=rules.mask_row)
+        h, b, m, r = rules.history, rules.bias_ids, rules.mask, rules.mask_row
+        if h is not None and (h.shape[0] != rows or h.get_device() != g):
+            _elsewhere(g, history=h)
+            _bad(f"history has {h.shape[0]} rows, the logits {rows}")
+        if b is not None and ((b.shape[0] != 1 and b.shape[0] != rows) or b.get_device() != g or rules.bias_values.get_device() != g):
+            _elsewhere(g, bias_ids=b, bias_values=rules.bias_values)
+            _bad(f"bias_ids has {b.shape[0]} rows, the logits {rows}")
+        if m is not None and (m.shape[1] != (classes + 31) // 32 or m.get_device() != g):
+            _elsewhere(g, mask=m)
+            _bad(f"mask has {m.shape[1]} words a row, expected {(classes + 31) // 32}")
+        if r is not None and (r.shape[0] != rows or r.get_device() != g):
+            _elsewhere(g, mask_row=r)
+            _bad(f"mask_row has {r.shape[0]} entries, expected {rows}")
         ref = rules.ref
-    _same_device(dev, target=target, logprobs=logprobs)
-    ws, nbytes = _scratch(dev, stream, 0 if workspace is not None else lb_logits_workspace(rows, classes), workspace, "lb_logits_adjust")
-    _call(dev, stream, "lb_logits_adjust", dt, rows, classes, logits.data_ptr(), stride, ref, _ptr(target), _ptr(logprobs), os,
-          _ptr(score), _ptr(lse), _ptr(ws), nbytes)
+    ws, nbytes, _held = _scratch(logits, stream, 0 if workspace is not None else lb_logits_workspace(rows, classes), workspace, "lb_logits_adjust")
+    _call(g, stream, "lb_logits_adjust", dt, rows, classes, logits.data_ptr(), stride, ref, _ptr(target), _ptr(logprobs), os,
+          _ptr(score), _ptr(lse), ws, nbytes)
     return logprobs, score, lse

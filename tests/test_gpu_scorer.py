@@ -234,8 +234,17 @@ ATTEND = [  # new, length, page, q heads, kv heads, D, window, type, padding row
     ([1] * 3, [1, 500, 31], 256, 2, 2, 256, 0, "bf16", 0),
     ([130], [400], 32, 4, 2, 128, 1, "f32", 0),
     ([1, 9], [3000, 1800], 64, 8, 8, 64, 0, "bf16", 0),
+    # prompts and single tokens in one batch: each by the kernel for its number of rows, the single ones by parts of their keys
+    ([1, 90, 0, 1, 33, 1], [2100, 200, 9, 40, 33, 1], 16, 4, 1, 128, 0, "bf16", 3),
+    ([200, 1, 17], [210, 1300, 17], 32, 4, 2, 256, 0, "bf16", 0),
+    ([17, 64, 65, 129, 1, 2, 3], [17, 70, 65, 500, 1, 64, 30], 64, 2, 2, 64, 40, "f16", 1),
+    ([150, 1], [333, 700], 16, 3, 1, 128, 64, "f32", 0),
+    ([70, 3], [90, 5], 16, 2, 1, 256, 2 ** 31 - 1, "f32", 0),
+    ([66, 1], [70, 1], 128, 5, 1, 256, 0, "f16", 0),
 ]
-PIECE = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -17, torch.float32: 2.0 ** -25}
+# What the probabilities' pieces leave: bf16 has 8 significant bits, so a piece is off by at most half a step, 2^-8 of
+# what it stands for, and 1, 2 and 3 pieces by 2^-8, 2^-16 and 2^-24.
+PIECE = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -16, torch.float32: 2.0 ** -24}
 
 
 def bounds(want, lse, mass, reach, dt, D, n):
@@ -288,7 +297,7 @@ def test_attend(case):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
-@pytest.mark.parametrize("new,D", [(1, 64), (12, 128), (40, 64)])
+@pytest.mark.parametrize("new,D", [(1, 64), (12, 128), (40, 64), (48, 128), (45, 256)])
 def test_attend_unseen_tokens_have_no_effect(t, new, D):
     """NaN keys and values past a row's position reach no row before them; those a row sees make it NaN."""
     rng = np.random.default_rng(8)
@@ -338,6 +347,39 @@ def test_attend_rows_that_see_nothing():
     b, bl = bounds(want, wl, mass, reach, torch.float32, 64, 40)
     close(out[1:2], want, b, "out")
     close(lse[1:2], wl, bl, "lse")
+
+
+def test_attend_leaves_rows_out_that_no_sequence_has():
+    """Starts that do not fit: the rows between the sequences, and those past max_new, stay as they were, with one
+    part of the keys and with several."""
+    rng = np.random.default_rng(15)
+    for length in (40, 2000):
+        R = ref.Ragged([2, 2], [length, 30], 16, 1, 64, seed=16)
+        for s in range(2):
+            R.put(s, randn(rng, R.length[s], 1, 64, dtype=torch.float64), randn(rng, R.length[s], 1, 64, dtype=torch.float64))
+        q = dev(randn(rng, 6, 2, 64))
+        for starts, fine, bad in (([0, 2, 6], [0, 1, 2, 3], True), ([1, 3, 5], [1, 2, 3, 4], False), ([0, -5, 4], [0, 1], True)):
+            word = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+            cache = lbm.KVCache(dev(R.pages), 16, 1, 64, flags=word)
+            batch = lbm.KVBatch(dev(torch.tensor(starts, dtype=torch.int32)), dev(R.lengths), dev(R.table), 6, 2)
+            say(f"[case] rows left out {length} {starts}")
+            out, lse = torch.full((6, 2, 64), 7.0, device="cuda:0"), torch.full((6, 2), 7.0, device="cuda:0")
+            lbm.lb_kv_attend(cache, batch, q, 1.0, out=out, lse=lse)
+            rest = [i for i in range(6) if i not in fine]
+            assert bool((out[rest] == 7.0).all()) and bool((lse[rest] == 7.0).all())
+            assert not bool((lse[fine] == 7.0).any())
+            assert cache.status() == (lbm.LB_KV_BAD_LENGTH if bad else 0)
+
+
+@pytest.mark.parametrize("starts", [[0, -5, 4], [7, 2, 4], [0, 3, 2], [0, 2, 9], [-2 ** 31, 2, 4]])
+def test_append_alone_reports_starts_that_do_not_fit(starts):
+    R = ref.Ragged([2, 2], [20, 30], 16, 1, 64, seed=6)
+    R.starts[:] = torch.tensor(starts, dtype=torch.int32)
+    cache, batch = handles(R)
+    k = torch.zeros(4, 1, 64, device="cuda:0")
+    say(f"[case] append starts {starts}")
+    lbm.lb_kv_append(cache, batch, None, k, k)
+    assert cache.status() == lbm.LB_KV_BAD_LENGTH
 
 
 def test_attend_large_scores():
@@ -644,3 +686,22 @@ def test_a_stream_of_the_callers():
     side.synchronize()
     for a, b in zip(want, outs()):
         assert torch.equal(a, b)
+
+
+def test_new_memory_belongs_to_the_call_s_stream():
+    """A block that torch's current stream has just let go of may still be in use by work queued there: a call on
+    another stream does not get it."""
+    side = torch.cuda.Stream()
+    logits, target = torch.zeros(64, 50000, device="cuda:0"), torch.zeros(64, dtype=torch.int32, device="cuda:0")
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        held = [torch.empty(64 * 50000, device="cuda:0"), torch.empty(64, device="cuda:0"), torch.empty(64, device="cuda:0")]
+        old = {t.data_ptr() for t in held}
+        del held
+        new = lbm.lb_logits_adjust(logits, target=target, stream=stream)
+        assert not old & {t.data_ptr() for t in new}
+        side.synchronize()
+        close(new[2], torch.full((64,), math.log(50000), dtype=torch.float64), 2.0 ** -18, "lse")
+    null = lbm.lb_logits_adjust(logits, target=target, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(null[2], new[2])

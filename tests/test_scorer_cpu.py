@@ -80,7 +80,7 @@ def test_caches_that_are_refused(over):
 
 @pytest.mark.parametrize("over", [dict(starts=None), dict(lengths=None), dict(pages=None), dict(n_seqs=-1), dict(n_rows=-1),
                                   dict(max_pages=0), dict(max_pages=1 << 27), dict(max_new=0), dict(n_rows=(1 << 28) + 1),
-                                  dict(n_seqs=(1 << 24) + 1)])
+                                  dict(n_seqs=(1 << 24) + 1), dict(n_rows=(1 << 24) + 1), dict(n_seqs=(1 << 22) + 1)])
 def test_batches_that_are_refused(over):
     assert refused(append(b=batch(**over)))
     assert refused(attend(b=batch(**over)))
@@ -96,7 +96,8 @@ def test_appends_that_are_refused(over):
 
 
 @pytest.mark.parametrize("over", [dict(dtype=5), dict(hq=0), dict(hq=3), dict(q=None), dict(o=None), dict(qs=200), dict(os_=257),
-                                  dict(o=AT + 2), dict(scale=math.nan), dict(scale=math.inf), dict(window=-1),
+                                  dict(o=AT + 2), dict(scale=math.nan), dict(scale=math.inf), dict(window=-1), dict(scale=3e38),
+                                  dict(c=cache(kv_heads=1024), hq=1024, qs=65536, os_=65536, b=batch(n_seqs=1 << 20, n_rows=1 << 20)),
                                   dict(c=cache(page_tokens=256), b=batch(max_pages=4096), ws=None),
                                   dict(c=cache(page_tokens=256), b=batch(max_pages=4096), nb=64),
                                   dict(c=cache(page_tokens=256), b=batch(max_pages=4096), ws=AT + 4)])
@@ -143,7 +144,7 @@ def rules(**over):
 
 
 @pytest.mark.parametrize("over", [dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.nan), dict(repetition=0.0),
-                                  dict(repetition=math.inf), dict(presence=math.nan), dict(frequency=math.inf),
+                                  dict(repetition=math.inf), dict(temperature=1e-39), dict(repetition=1e-40), dict(presence=math.nan), dict(frequency=math.inf),
                                   dict(history=AT, history_width=-1), dict(history=AT, history_width=4097),
                                   dict(bias_ids=AT, bias_width=4), dict(bias_ids=AT, bias_values=AT, bias_width=2049, history=AT, history_width=2048),
                                   dict(mask=AT), dict(mask=AT, mask_rows=2)])
