@@ -479,11 +479,16 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// 255 in each byte that is 255, else 0
-__device__ __forceinline__ uint32_t bytes_255(uint32_t w) {
-  const uint32_t all = (w & 0x7F7F7F7Fu) + 0x01010101u & w & 0x80808080u;  // bit 7: the low seven bits carry into it, and it is set
-  return (all >> 7) * 255u;
+// The value itself, which the compiler does not know: what is computed from it
+// stays behind the branch that it stands behind, and is not done ahead for all.
+template <typename I>
+__device__ __forceinline__ I behind_branch(I x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
+
+// bit 7 of each byte that is 255: its low seven bits carry into it, and it is set
+__device__ __forceinline__ uint32_t carry_255(uint32_t w) { return (w & 0x7F7F7F7Fu) + 0x01010101u & w & 0x80808080u; }
 
 // The pages of a key range: tiles of 32 tokens from `begin` on, of which a
 // wavefront takes every `step`-th.  Lane i holds the pages (of both halves of 16
@@ -511,6 +516,8 @@ struct Pages {
       if (page0 >= n_pages) page0 = -1;
       if (page1 >= n_pages) page1 = -1;
     }
+    // no load is under way when the branches join: else every tile would wait here for all that are (vmcnt 0)
+    __builtin_amdgcn_s_waitcnt(0x0F70);
   }
 
   // the pages of tile t's halves, -1: none
@@ -593,41 +600,48 @@ struct Keys {
   }
 };
 
-// The values' scales of a tile, tokens from `end` on (and of halves that do not
-// exist) as 0, whatever the cache holds there, and blocks of NaN too: what is NaN
-// is left in `nan`, 255 a byte.
+// The scale operand of byte i of a word of scale bytes.  The conversion takes the
+// exponent bits of its operand and no others (tried with every byte and code on
+// gfx950), so the other bytes need not be cleared.
+__device__ __forceinline__ float scale_at(uint32_t word, int i) { return __uint_as_float(i == 3 ? word >> 1 : word << (23 - 8 * i)); }
+
+// The values' scales of a tile; tokens from `end` on, and of halves that do not
+// exist, get the byte 0, whatever the cache holds there, and so do blocks of NaN:
+// which these are is left in `nan`, 255 a byte.
 struct ValueScales {
   uint32_t bytes[2], nan[2];
-  float s[2][4];
+  bool any_nan;  // in some lane
 
-  __device__ __forceinline__ ValueScales(const uint32_t (&vs)[2], int32_t tb, int32_t end, int ok, int j) {
+  __device__ __forceinline__ ValueScales(const uint32_t (&vs)[2], bool whole, int32_t tb, int32_t end, int ok, int j) {
     bytes[0] = vs[0], bytes[1] = vs[1];
-    if (ok != 3 || tb + 32 > end) {
-      asm volatile("");  // a branch: most tiles are whole
+    if (!whole) {
+      const int32_t at = behind_branch(tb);  // most tiles are whole
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int32_t left = ok >> u & 1 ? end - (tb + 16 * u + 4 * j) : 0;
+        const int32_t left = ok >> u & 1 ? end - (at + 16 * u + 4 * j) : 0;
         bytes[u] = left >= 4 ? bytes[u] : left <= 0 ? 0u : bytes[u] & ((1u << (8 * left)) - 1u);
       }
     }
+    nan[0] = nan[1] = 0;
+    any_nan = __any((carry_255(bytes[0]) | carry_255(bytes[1])) != 0);
+    if (any_nan) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      nan[u] = bytes_255(bytes[u]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[u][i] = scale_of((bytes[u] & ~nan[u]) >> (8 * i) & 255u);
+      for (int u = 0; u < 2; ++u) {
+        nan[u] = (carry_255(behind_branch(bytes[u])) >> 7) * 255u;
+        bytes[u] &= ~nan[u];
+      }
     }
   }
-  __device__ __forceinline__ bool any_nan() const { return __any((nan[0] | nan[1]) != 0); }
 
   // one word of values (a channel pair of four tokens) of each half, as bf16: [half][token] channel pairs
   __device__ __forceinline__ void convert(uint32_t w0, uint32_t w1, uint32_t (&y)[2][4]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const uint32_t w = u ? w1 : w0;
-      y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][0], 0));
-      y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][1], 1));
-      y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][2], 2));
-      y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s[u][3], 3));
+      y[u][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_at(bytes[u], 0), 0));
+      y[u][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_at(bytes[u], 1), 1));
+      y[u][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_at(bytes[u], 2), 2));
+      y[u][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale_at(bytes[u], 3), 3));
     }
   }
 };
@@ -659,11 +673,10 @@ struct Rows {
     return ok == 3 && tb + 31 <= p_min && tb + 32 <= end && (window <= 0 || tb > p_max - window);
   }
 
-  // The probabilities of a tile's tokens as matrix operands, and their sums.
-  // key(u, c): channels j D/4 + 8 c .. + 7 of the lane's token in half u.
+  // Scores of a tile's tokens, before the scale; key(u, c): channels j D/4 + 8 c
+  // .. + 7 of the lane's token in half u.
   template <typename Key>
-  __device__ __forceinline__ void weigh(Key&& key, int32_t tb, int ok, int j, bf16x8 (&pf)[QT][NP]) {
-    f32x4 acc[QT][2];
+  __device__ __forceinline__ void score(Key&& key, f32x4 (&acc)[QT][2]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -677,29 +690,44 @@ struct Rows {
           for (int p = 0; p < NP; ++p) acc[t][u] = mfma(kf, q[t][c][p], acc[t][u]);
       }
     }
+  }
+
+  // The tokens' probabilities as matrix operands, and their sums.
+  __device__ __forceinline__ void weigh(f32x4 (&acc)[QT][2], int32_t tb, int ok, int j, bf16x8 (&pf)[QT][NP]) {
     if (!inner(tb, ok)) {
-      asm volatile("");  // a branch: most tiles are whole
+      const int32_t at = behind_branch(tb);  // most tiles are whole
 #pragma unroll
       for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u) {
+          int32_t lo, hi;
+          range(t, at + 16 * u + 4 * j, ok >> u & 1, lo, hi);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!seen(t, tb + 16 * u + 4 * j + i, ok >> u & 1)) acc[t][u][i] = -__builtin_inff();
+            if (i < lo || i > hi) acc[t][u][i] = -__builtin_inff();
+        }
     }
+    float top[QT];
+    bool past = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float top = larger(larger(larger(acc[t][0][0], acc[t][0][1]), larger(acc[t][0][2], acc[t][0][3])),
-                         larger(larger(acc[t][1][0], acc[t][1][1]), larger(acc[t][1][2], acc[t][1][3])));
-      top *= scale2;
-      if (__any(top > m[t] + kSlack)) {
-        const float mx = fmaxf(m[t], row_max(top));
+      top[t] = scale2 * larger(larger(larger(acc[t][0][0], acc[t][0][1]), larger(acc[t][0][2], acc[t][0][3])),
+                               larger(larger(acc[t][1][0], acc[t][1][1]), larger(acc[t][1][2], acc[t][1][3])));
+      past |= top[t] > m[t] + kSlack;
+    }
+    if (__any(past)) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float mx = fmaxf(m[t], row_max(top[t]));
         const float fade = mx == m[t] ? 1.0f : __builtin_amdgcn_exp2f(m[t] - mx);
         m[t] = mx;
         l[t] *= fade;
 #pragma unroll
         for (int c = 0; c < VC; ++c) o[t][c] *= fade;
       }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
       const float base = m[t] == -__builtin_inff() ? 0.0f : m[t];  // nothing seen yet: every exponent is -infinity
       float p[8];
 #pragma unroll
@@ -721,14 +749,16 @@ struct Rows {
 
   // One tile of keys and values.
   __device__ __forceinline__ void take(const Tile<D>& X, int32_t tb, int ok, int j) {
+    f32x4 acc[QT][2];
     bf16x8 pf[QT][NP];
-    weigh(
+    score(
         [&](int u, int c) {
           // channels j D/4 + 8 c .. + 7 lie in block (8 c) / 32 of the quarter (D = 256 has two there)
-          return bf16_of(X.k[u][c], scale_of(D == 256 ? (X.ks[u] >> (c < KC / 2 ? 0 : 8)) & 255u : X.ks[u]));
+          return bf16_of(X.k[u][c], scale_at(X.ks[u], D == 256 && c >= KC / 2 ? 1 : 0));
         },
-        tb, ok, j, pf);
-    const ValueScales V(X.vs, tb, end, ok, j);
+        acc);
+    weigh(acc, tb, ok, j, pf);
+    const ValueScales V(X.vs, ok == 3 && tb + 32 <= end, tb, end, ok, j);
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {
       uint32_t y[2][4];
@@ -736,27 +766,34 @@ struct Rows {
       add_channel(2 * w, channel(y, 0), pf);
       add_channel(2 * w + 1, channel(y, 1), pf);
     }
-    if (V.any_nan()) spread_nan(V.nan, tb, ok, j);
+    if (V.any_nan) spread_nan(V.nan, tb, ok, j);
   }
 
-  __device__ __forceinline__ bool seen(int t, int32_t tok, bool ok) const {
-    return ok && tok < end && tok <= pos[t] && (window <= 0 || tok > pos[t] - window);
+  // the tokens tok + lo .. tok + hi are those that row t sees
+  __device__ __forceinline__ void range(int t, int32_t tok, bool ok, int32_t& lo, int32_t& hi) const {
+    hi = ok ? min(pos[t], end - 1) - tok : -1;
+    lo = window > 0 ? pos[t] - window + 1 - tok : 0;
   }
 
   // A block of NaN reaches the rows that see its token, and no other: 0 * NaN in
   // the products would reach all of them.  So a product of what is NaN with what
   // is seen says which results it reaches.
   __device__ __forceinline__ void spread_nan(const uint32_t (&nan)[2], int32_t tb, int ok, int j) {
-    asm volatile("");  // a branch: there is no such block as a rule
+    const int32_t at = behind_branch(tb);  // there is no such block as a rule
+    const uint32_t word[2] = {behind_branch(nan[0]), behind_branch(nan[1])};
     bf16x8 bad;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bad[i] = static_cast<__bf16>(nan[i >> 2] >> (8 * (i & 3)) & 1u ? 1.0f : 0.0f);
+    for (int i = 0; i < 8; ++i) bad[i] = static_cast<__bf16>(word[i >> 2] >> (8 * (i & 3)) & 1u ? 1.0f : 0.0f);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       bf16x8 vis;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        vis[i] = static_cast<__bf16>(seen(t, tb + 16 * (i >> 2) + 4 * j + (i & 3), ok >> (i >> 2) & 1) ? 1.0f : 0.0f);
+      for (int u = 0; u < 2; ++u) {
+        int32_t lo, hi;
+        range(t, at + 16 * u + 4 * j, ok >> u & 1, lo, hi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vis[4 * u + i] = static_cast<__bf16>(i >= lo && i <= hi ? 1.0f : 0.0f);
+      }
       const f32x4 hit = mfma(bad, vis, f32x4{0, 0, 0, 0});
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -772,7 +809,8 @@ struct Rows {
     int ok = t < t_hi ? K.load(t, X, flags) : 0;
     for (; t < t_hi; t += K.P.step) {
       const int next = t + K.P.step < t_hi ? K.load(t + K.P.step, Y, flags) : 0;
-      take(X, K.P.begin + t * 32, ok, j);
+      const int32_t tb = K.P.begin + t * 32;
+      take(X, tb, ok, j);
       X = Y;
       ok = next;
     }
@@ -809,17 +847,21 @@ __device__ __forceinline__ Job few_job(const AttendArgs& A, uint32_t job) {
   if (w.R > kFewRows) w.R = 0;  // the many-row kernel's
   return w;
 }
+// every sequence has a job of tile 0 and head 0
+__device__ __forceinline__ void report(const AttendArgs& A, const Job& w) {
+  if (w.q.bad && w.tile == 0 && w.h == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+}
 
 // Rows r0 .. r0 + 16 QT - 1 of the job into a wavefront's state; false: there are none.
 template <int D, typename T, int QT>
 __device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32_t r0, Rows<D, Pieces<T>::n, QT>& S, int n, int j) {
-  if (r0 >= w.R) return false;
   S.scale2 = fabsf(A.scale2);
   float sign = A.scale2 < 0.0f ? -1.0f : 1.0f;
   if (A.scale2 == 0.0f) sign = 0.0f, S.scale2 = 1.0f;
   S.window = A.window;
-  S.p_min = w.q.pos0 + r0 / w.G;
-  S.p_max = w.q.pos0 + (min(w.R, r0 + 16 * QT) - 1) / w.G;
+  const bool have = r0 < w.R;
+  S.p_min = have ? w.q.pos0 + r0 / w.G : -1;
+  S.p_max = have ? w.q.pos0 + (min(w.R, r0 + 16 * QT) - 1) / w.G : -1;
   S.end = min(w.q.len, S.p_max + 1);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -840,7 +882,7 @@ __device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32
       split8<Pieces<T>::n>(x, S.q[t][c]);
     }
   }
-  return true;
+  return have;
 }
 
 template <int N, typename T>
@@ -864,16 +906,55 @@ __device__ __forceinline__ void store_channels(T* dst, const float (&x)[N]) {
 __device__ __forceinline__ float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }  // l may be NaN
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -__builtin_inff() : (m + log2f(l)) * 0.6931471805599453f; }
 
+// The results of a wavefront's rows r0 .. r0 + 16 QT - 1 that have seen all of their keys.
+template <int D, typename T, int QT>
+__device__ __forceinline__ void store_rows(const AttendArgs& A, const Job& w, int32_t r0, const Rows<D, Pieces<T>::n, QT>& S, int n, int j) {
+  constexpr int VC = D / 16;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const float total = row_sum(S.l[t]), inv = inverse(total);
+    const int32_t r = r0 + 16 * t + n;
+    if (r >= w.R) continue;
+    const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
+    const int32_t hq = w.h * w.G + r % w.G;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[VC];
+#pragma unroll
+      for (int c = 0; c < VC; ++c) x[c] = S.o[t][c][i] * inv;
+      store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + (4 * j + i) * (D / 16), x);
+    }
+    if (A.lse && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(S.m[t], total);
+  }
+}
+
+// Few query rows and short key ranges, but many of them: a wavefront takes a job on
+// its own, and has nothing to join.
+template <int D, typename T>
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend_short(AttendArgs A) {
+  const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
+  const uint32_t job = blockIdx.x * 4 + wave_index();
+  if (job >= static_cast<uint32_t>(A.kv.n_seqs * A.tiles * A.kv.kv_heads)) return;
+  const Job w = few_job(A, job);
+  if (lane == 0) report(A, w);
+  Rows<D, Pieces<T>::n, 1> S;
+  if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
+  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
+  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
+  S.sweep(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
+  store_rows<D, T, 1>(A, w, w.tile * 16, S, n, j);
+}
+
 // Few query rows: a workgroup takes 16 rows and one part of their key range; its
 // four wavefronts take every fourth tile and join at the end.
 template <int D, typename T>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  check_sequence(A.kv, blockIdx.x);
   const uint32_t job = blockIdx.x / A.splits;
   const int32_t split = static_cast<int32_t>(blockIdx.x % A.splits);
   const Job w = few_job(A, job);
+  if (split == 0 && threadIdx.x == 0) report(A, w);
   Rows<D, Pieces<T>::n, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
@@ -932,15 +1013,20 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
 
 // Many query rows: each of the four wavefronts has 16 QT rows of its own, and all
 // take the same tiles.  A tile is converted to bf16 operands once, a quarter by
-// each wavefront, and goes through LDS in the order in which lanes read it; the
-// conversion of the next one and the loads of the one after it are made while a
-// tile is used, with one barrier a tile.
+// each wavefront, and goes through LDS in the order in which lanes read it.  While
+// the probabilities of tile t are computed, its values come from LDS; the products
+// with them hide the reading of the keys of t + 1, whose scores follow.  Later keys
+// and values are converted meanwhile, and what the step after needs is on its way
+// from memory.  A ring of 2 A tiles has a barrier every A tiles: at step t the keys
+// of t + 1 and the values of t are read, made A steps or more before, and those of t
+// + 1 + A and t + A are made, in places that were last read A steps or more before.
 template <int D>
 struct Shared {
   static constexpr int KC = D / 32, VC = D / 16;
-  bf16x8 key[2][2 * KC][64], value[2][VC][64];  // [tile % 2][half and channels, or channel][lane]
-  uint32_t nan[2][2][64];
-  int32_t any_nan[2];
+  static constexpr int A = D <= 128 ? 2 : 1, N = 2 * A;  // at most 64 KB: two workgroups a CU
+  bf16x8 key[N][2 * KC][64], value[N][VC][64];  // [tile % N][half and channels, or channel][lane]
+  uint32_t nan[N][2][64];
+  int32_t any_nan[N];
 };
 
 template <int D>
@@ -952,7 +1038,10 @@ struct Maker {
   uint32_t k_at, v_at, ks_at, vs_at;
   int u;  // the half whose keys are this wavefront's
   uint32_t k[F], v[2][W], ks, vs[2];
-  int ok;
+  int ok;                    // the halves there are of the tile whose values are held
+  const uint8_t* half[2];    // where the halves start of the tile whose keys are held: codes and, P D bytes on, scales
+  const uint8_t* scales[2];
+  int there = 0;             // the halves there are of that tile
 
   __device__ __forceinline__ Maker(const KvArgs& A, int32_t s, int32_t h, int32_t begin, int32_t end, int wave, int n, int j)
       : P(A, s, begin, end, 1), u(wave >> 1), ks(0), ok(0) {
@@ -970,30 +1059,39 @@ struct Maker {
     vs[0] = vs[1] = 0;
   }
 
-  __device__ __forceinline__ void load(int32_t t, uint32_t* flags) {
+  __device__ __forceinline__ void load_keys(int32_t t, uint32_t* flags) {
     int32_t page[2];
     P.of(t, page, flags);
-    ok = (page[0] >= 0 ? 1 : 0) | (page[1] >= 0 ? 2 : 0);
-    if (const int32_t mine = u ? page[1] : page[0]; mine >= 0) {
-      const uint8_t* at = base + mine * page_bytes;
-      load_words<F>(at + P.slot(t, u) * (D / 2) + k_at, k);
-      ks = at[P.slot(t, u) * (D / 32) + ks_at];
+    there = (page[0] >= 0 ? 1 : 0) | (page[1] >= 0 ? 2 : 0);
+    const int32_t slot = P.slot(t, 0), next = P.slot(t, 1);
+    half[0] = base + page[0] * page_bytes;
+    half[1] = page[1] == page[0] ? half[0] : base + page[1] * page_bytes;
+    scales[0] = half[0] + slot * (D / 32), scales[1] = half[1] + next * (D / 32);
+    half[0] += slot * (D / 2), half[1] += next * (D / 2);
+    if (there >> u & 1) {  // else what the registers hold stays unseen
+      load_words<F>((u ? half[1] : half[0]) + k_at, k);
+      ks = (u ? scales[1] : scales[0])[ks_at];
     }
+  }
+  // of the tile that load_keys loaded last
+  __device__ __forceinline__ void load_values() {
+    ok = there;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      if (page[x] < 0) continue;
-      const uint8_t* at = base + page[x] * page_bytes;
-      load_words<W>(at + P.slot(t, x) * (D / 2) + v_at, v[x]);
-      vs[x] = *reinterpret_cast<const uint32_t*>(at + P.slot(t, x) * (D / 32) + vs_at);
+      if (!(ok >> x & 1)) continue;
+      load_words<W>(half[x] + v_at, v[x]);
+      vs[x] = *reinterpret_cast<const uint32_t*>(scales[x] + vs_at);
     }
   }
 
   // what has been loaded, into buffer b; tb: the tile's first token
-  __device__ __forceinline__ void make(Shared<D>& L, int b, int32_t tb, int wave, int lane) const {
+  __device__ __forceinline__ void make_keys(Shared<D>& L, int b, int wave, int lane) const {
     const float s = scale_of(ks);
 #pragma unroll
     for (int i = 0; i < F; ++i) L.key[b][wave * F + i][lane] = bf16_of(k[i], s);
-    const ValueScales V(vs, tb, P.end, ok, lane >> 4);
+  }
+  __device__ __forceinline__ void make_values(Shared<D>& L, int b, int32_t tb, int wave, int lane) const {
+    const ValueScales V(vs, ok == 3 && tb + 32 <= P.end, tb, P.end, ok, lane >> 4);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       uint32_t y[2][4];
@@ -1006,19 +1104,25 @@ struct Maker {
       }
     }
     if (wave == 0) {  // its lanes have the scales of all blocks
-      const bool any = V.any_nan();
-      if (any) L.nan[b][0][lane] = V.nan[0], L.nan[b][1][lane] = V.nan[1];
-      if (lane == 0) L.any_nan[b] = any;
+      if (V.any_nan) L.nan[b][0][lane] = V.nan[0], L.nan[b][1][lane] = V.nan[1];
+      if (lane == 0) L.any_nan[b] = V.any_nan;
     }
   }
 };
 
+// Operands that the many-row kernel reads ahead: as many of N as the registers hold beside its state.
+constexpr int ahead(int D, int pieces, int QT, int N) {
+  const int state = 4 * QT * (D / 16 + D / 32 * pieces + 2 + pieces) + 56, room = (256 - state) / 8;
+  return room >= N ? N : room >= N / 2 ? N / 2 : room >= 4 ? 4 : 2;
+}
+
 template <int D, typename T, int QT>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows(AttendArgs A) {
-  constexpr int VC = D / 16, NP = Pieces<T>::n, per = 64 * QT;
+  constexpr int KC = D / 32, VC = D / 16, NP = Pieces<T>::n, per = 64 * QT;
+  constexpr int KA = ahead(D, NP, QT, 2 * KC), VA = ahead(D, NP, QT, VC);
   __shared__ Shared<D> L;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  check_sequence(A.kv, blockIdx.x);
+  if (!A.few) check_sequence(A.kv, blockIdx.x);
   Job w;
   w.G = A.kv.q_heads / A.kv.kv_heads;
   w.h = static_cast<int32_t>(blockIdx.x % A.kv.kv_heads);
@@ -1029,61 +1133,72 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows
   const int32_t tiles_of_rows = (w.R + per - 1) / per;
   if (w.tile < 0 || w.tile >= tiles_of_rows) return;
   w.tile = tiles_of_rows - 1 - w.tile;  // the last rows see most keys: they go first
+  // a wavefront without rows goes along, and sees nothing
   Rows<D, NP, QT> S;
   const bool have = rows_of<D, T, QT>(A, w, (w.tile * 4 + wave) * 16 * QT, S, n, j);
   // the key range of all four wavefronts' rows
   const int32_t first = w.q.pos0 + w.tile * per / w.G, last = w.q.pos0 + (min(w.R, (w.tile + 1) * per) - 1) / w.G;
   const int32_t begin = A.window > 0 ? max(0, first - A.window + 1) & ~31 : 0, end = min(w.q.len, last + 1);
   const int32_t tiles = end > begin ? (end - begin + 31) >> 5 : 0;
-  Maker<D> M(A.kv, w.s, w.h, begin, end, wave, n, j);
-  int ok = 0;
   if (tiles > 0) {
-    M.load(0, A.kv.flags);
-    M.make(L, 0, begin, wave, lane);
-    ok = M.ok;
-    if (tiles > 1) M.load(1, A.kv.flags);
-  }
-  __syncthreads();
-  for (int32_t t = 0; t < tiles; ++t) {
-    const int b = t & 1;
-    const int32_t tb = begin + t * 32;
-    int next = 0;
-    if (t + 1 < tiles) {
-      M.make(L, b ^ 1, tb + 32, wave, lane);
-      next = M.ok;
-      if (t + 2 < tiles) M.load(t + 2, A.kv.flags);
-    }
-    // a row of this wavefront may see the tile
-    if (have && tb <= S.p_max && (S.window <= 0 || tb + 31 > S.p_min - S.window)) {
-      bf16x8 pf[QT][NP];
-      S.weigh([&](int u, int c) { return L.key[b][u * (D / 32) + c][lane]; }, tb, ok, j, pf);
+    Maker<D> M(A.kv, w.s, w.h, begin, end, wave, n, j);
+    f32x4 acc[QT][2];
+    bf16x8 kf[KA], vf[VA];
+    const auto read_keys = [&](int b) {
 #pragma unroll
-      for (int c = 0; c < VC; ++c) S.add_channel(c, L.value[b][c][lane], pf);
-      if (__builtin_amdgcn_readfirstlane(L.any_nan[b])) {
-        const uint32_t nan[2] = {L.nan[b][0][lane], L.nan[b][1][lane]};
-        S.spread_nan(nan, tb, ok, j);
-      }
+      for (int i = 0; i < KA; ++i) kf[i] = L.key[b][i][lane];
+    };
+    const auto score = [&](int b) {
+      S.score([&](int u, int c) { return u * KC + c < KA ? kf[u * KC + c] : L.key[b][u * KC + c][lane]; }, acc);
+    };
+    constexpr int S_A = Shared<D>::A, N = Shared<D>::N;
+    int ok[S_A + 1];  // the halves there are of tiles t .. t + A
+#pragma unroll
+    for (int i = 0; i <= S_A; ++i) {
+      M.load_keys(min(i, tiles - 1), A.kv.flags);
+      M.make_keys(L, i, wave, lane);
+      M.load_values();
+      ok[i] = M.ok;
+      if (i < S_A) M.make_values(L, i, begin + 32 * i, wave, lane);
     }
-    ok = next;
+    M.load_keys(min(S_A + 1, tiles - 1), A.kv.flags);
     __syncthreads();
-  }
-  if (!have) return;
+    read_keys(0);
+    score(0);
+    __syncthreads();  // before other keys go where those of tile 0 are
+    // past the last tile the last one is made again, and nobody reads it
+#pragma unroll S_A
+    for (int32_t t = 0; t < tiles; ++t) {
+      const int b = t & (N - 1);
+      const int32_t tb = begin + t * 32;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const float total = row_sum(S.l[t]), inv = inverse(total);
-    const int32_t r = (w.tile * 4 + wave) * 16 * QT + 16 * t + n;
-    if (r >= w.R) continue;
-    const int64_t row = w.q.row0 + static_cast<int64_t>(r / w.G);
-    const int32_t hq = w.h * w.G + r % w.G;
+      for (int c = 0; c < VA; ++c) vf[c] = L.value[b][c][lane];
+      const int32_t flag = L.any_nan[b];
+      M.make_keys(L, (t + 1 + S_A) & (N - 1), wave, lane);
+      M.make_values(L, (t + S_A) & (N - 1), tb + 32 * S_A, wave, lane);
+      M.load_values();
+      M.load_keys(min(t + 2 + S_A, tiles - 1), A.kv.flags);
+      bf16x8 pf[QT][NP];
+      const int here = ok[0];
+      S.weigh(acc, tb, here, j, pf);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float x[VC];
+      for (int i = 0; i < S_A; ++i) ok[i] = ok[i + 1];
+      ok[S_A] = M.ok;
+      const bool any_nan = __builtin_amdgcn_readfirstlane(flag) != 0;
+      __builtin_amdgcn_sched_barrier(0);
+      read_keys((t + 1) & (N - 1));
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < VC; ++c) x[c] = S.o[t][c][i] * inv;
-      store_channels<VC>(static_cast<T*>(A.out) + row * A.out_stride + hq * D + (4 * j + i) * (D / 16), x);
+      for (int c = 0; c < VC; ++c) S.add_channel(c, c < VA ? vf[c] : L.value[b][c][lane], pf);
+      if (any_nan) {
+        const uint32_t nan[2] = {L.nan[b][0][lane], L.nan[b][1][lane]};
+        S.spread_nan(nan, tb, here, j);
+      }
+      score((t + 1) & (N - 1));
+      if (S_A == 1 || (t & (S_A - 1)) == S_A - 1) __syncthreads();
     }
-    if (A.lse && j == 0) A.lse[row * A.kv.q_heads + hq] = lse_of(S.m[t], total);
   }
+  if (have) store_rows<D, T, QT>(A, w, (w.tile * 4 + wave) * 16 * QT, S, n, j);
 }
 
 // Joins the parts of a row's key range: a workgroup per row of the few-row
@@ -1170,6 +1285,10 @@ hipError_t attend(const AttendArgs& A, hipStream_t st) {
     if (e != hipSuccess || !A.few) return e;
   }
   const int64_t jobs = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads;
+  if (A.alone) {
+    k_attend_short<D, T><<<dim3(static_cast<unsigned>((jobs + 3) / 4)), 256, 0, st>>>(A);
+    return hipGetLastError();
+  }
   k_attend<D, T><<<dim3(static_cast<unsigned>(jobs * A.splits)), 256, 0, st>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.splits == 1) return e;
@@ -1193,8 +1312,11 @@ hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(attend); }
 
 // How a call is cut up.  Sequences with at most kFewRows query rows a KV head:
-// tiles of 16 rows, and parts of the key range so that about eight workgroups a CU
-// exist, each with 16 tiles of keys at least.  The others: a workgroup takes the
+// tiles of 16 rows, and parts of the key range so that about three workgroups a CU
+// exist (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8
+// heads take 99 us with them, 101 with six, 106 with eight), each with 16 tiles of
+// keys at least; where there are many such jobs with at most 16 tiles of keys, a
+// wavefront takes one alone (ALONE_FIGURES).  The others: a workgroup takes the
 // rows of its four wavefronts, and the workgroups are numbered as append's units
 // are, so that a ragged batch has no more than one idle one a sequence and head.  A
 // batch that may hold both gets both kernels, each of which leaves the other's
@@ -1214,7 +1336,8 @@ AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   p.part_rows = static_cast<int32_t>(most < 16 ? most : 16);
   const int64_t jobs = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;
   const int64_t tokens = static_cast<int64_t>(kv.max_pages) << kv.page_shift;
-  int64_t s = (2048 + jobs - 1) / jobs;
+  p.alone = tokens <= 512 && jobs > 2048;
+  int64_t s = (768 + jobs - 1) / jobs;
   s = s < tokens / 512 ? s : tokens / 512;
   p.splits = static_cast<int32_t>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
   if (p.splits > 1) {

@@ -29,41 +29,45 @@ __device__ __forceinline__ const uint32_t* mask_of(const LogitArgs& A, int64_t r
   return k >= 0 && k < A.r.mask_rows ? A.r.mask + k * ((A.classes + 31) / 32) : nullptr;
 }
 
-// The rules for one class, in the order that the header gives.  The divisions
-// are products with the rounded reciprocals: one rounding of 2^-24 more.
+// The rules for one class up to the temperature, in the order that the header
+// gives.  The division by the repetition penalty is a product with its rounded
+// reciprocal: one rounding of 2^-24 more.
 struct Rules {
-  float inv_temperature, repetition, inv_repetition, presence, frequency;
+  float repetition, inv_repetition, presence, frequency;
   __device__ __forceinline__ explicit Rules(const lb_logit_rules& r)
-      : inv_temperature(1.0f / r.temperature), repetition(r.repetition), inv_repetition(1.0f / r.repetition),
-        presence(r.presence), frequency(r.frequency) {}
+      : repetition(r.repetition), inv_repetition(1.0f / r.repetition), presence(r.presence), frequency(r.frequency) {}
   __device__ __forceinline__ float operator()(float x, int32_t count, float bias) const {
     if (count) x = x * (x > 0.0f ? inv_repetition : repetition) - presence - frequency * static_cast<float>(count);
-    return (x + bias) * inv_temperature;
+    return x + bias;
   }
 };
 
-// (m, l): a maximum and the sum of exp2(log2(e) (z - m)); nothing yet: (-inf, 0)
+// The temperature goes into the exponent: with k = log2(e) / temperature, rounded, a
+// term is 2^(k (x - m)), m the largest logit before the temperature.  What k lacks
+// (2^-24 of it, as the rounded quotient by the temperature would) is that part of a
+// difference between logits, not of the logits; and no logit is scaled, so those of
+// the type's lowest value stay finite.  A row's sum is (m, l); nothing yet: (-inf, 0).
 struct Sum {
   float m, l;
 };
 // what exponents are taken relative to: an infinite maximum would make inf - inf of them
 __device__ __forceinline__ float safe(float m) { return __builtin_isinf(m) ? 0.0f : m; }
-__device__ __forceinline__ float exp_of(float z, float base) { return __builtin_amdgcn_exp2f((z - base) * kLog2e); }
-__device__ __forceinline__ void join(Sum& a, float m2, float l2) {
+__device__ __forceinline__ float term(float x, float base, float k) { return __builtin_amdgcn_exp2f((x - base) * k); }
+__device__ __forceinline__ void join(Sum& a, float m2, float l2, float k) {
   const float m = fmaxf(a.m, m2), base = safe(m);
-  a.l = a.l * exp_of(a.m, base) + l2 * exp_of(m2, base);
+  a.l = a.l * term(a.m, base, k) + l2 * term(m2, base, k);
   a.m = m;
 }
-// n values at once: one rescaling of the sum
+// n logits at once: one rescaling of the sum
 template <int n>
-__device__ __forceinline__ void add(Sum& a, const float (&z)[n]) {
+__device__ __forceinline__ void add(Sum& a, const float (&x)[n], float k) {
   float m = a.m;
 #pragma unroll
-  for (int i = 0; i < n; ++i) m = fmaxf(m, z[i]);
+  for (int i = 0; i < n; ++i) m = fmaxf(m, x[i]);
   const float base = safe(m);
-  float l = a.l * exp_of(a.m, base);
+  float l = a.l * term(a.m, base, k);
 #pragma unroll
-  for (int i = 0; i < n; ++i) l += exp_of(z[i], base);
+  for (int i = 0; i < n; ++i) l += term(x[i], base, k);
   a.l = l;
   a.m = m;
 }
@@ -91,33 +95,37 @@ __device__ __forceinline__ float over_lanes(float x, F f) {
   }
   return x;
 }
-__device__ __forceinline__ Sum block_sum(Sum s) {
+__device__ __forceinline__ Sum block_sum(Sum s, float k) {
   __shared__ float sm[4], sl[4];
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const float m2 = __shfl_xor(s.m, d), l2 = __shfl_xor(s.l, d);
-    join(s, m2, l2);
+    join(s, m2, l2, k);
   }
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s.m, sl[threadIdx.x >> 6] = s.l;
   __syncthreads();
   Sum t{sm[0], sl[0]};
 #pragma unroll
-  for (int w = 1; w < 4; ++w) join(t, sm[w], sl[w]);
+  for (int w = 1; w < 4; ++w) join(t, sm[w], sl[w], k);
   return t;
 }
-// The log-sum-exp as maximum and rest: z - lse is taken as (z - m) - rest, which
-// stays right where m is so large that m + rest is m.
+// The log-sum-exp as its reference (a logit) and the rest (a power of two): log p =
+// ln2 (k (x - m) - rest) stays right where m is so large that m + rest is m.
 struct Lse {
   float m, rest;
+  __device__ __forceinline__ float value(float temperature) const { return m / temperature + rest * kLn2; }
 };
-__device__ __forceinline__ Lse log_sum(Sum s) { return {safe(s.m), s.l == 0.0f ? -__builtin_inff() : log2f(s.l) * kLn2}; }
-__device__ __forceinline__ float log_prob(float z, Lse lse) { return z == -__builtin_inff() ? z : (z - lse.m) - lse.rest; }
+__device__ __forceinline__ Lse log_sum(Sum s) { return {safe(s.m), s.l == 0.0f ? -__builtin_inff() : log2f(s.l)}; }
+__device__ __forceinline__ float log_prob(float x, float k, Lse lse) {
+  return x == -__builtin_inff() ? x : ((x - lse.m) * k - lse.rest) * kLn2;
+}
 
-__device__ __forceinline__ void finish(const LogitArgs& A, int64_t row, Lse lse, float zt) {
-  if (A.lse) A.lse[row] = lse.m + lse.rest;
+// xt: the target's logit after the rules up to the temperature
+__device__ __forceinline__ void finish(const LogitArgs& A, int64_t row, Lse lse, float xt, float k) {
+  if (A.lse) A.lse[row] = lse.value(A.r.temperature);
   if (!A.score) return;
   const int32_t t = A.target[row];
-  A.score[row] = t < 0 ? 0.0f : t >= A.classes ? __builtin_nanf("") : log_prob(zt, lse);
+  A.score[row] = t < 0 ? 0.0f : t >= A.classes ? __builtin_nanf("") : log_prob(xt, k, lse);
 }
 
 // ------------------------------------------------------------------ long rows
@@ -128,7 +136,7 @@ struct Slot {
   int32_t id;     // -1: empty
   int32_t count;  // occurrences in the history
   int32_t bias;   // place in the bias list + 1, 0: none
-  float z;        // the class's logit after the rules
+  float x;        // the class's logit after the rules up to the temperature
 };
 
 // A part of a row: the classes lo .. hi - 1, in chunks of eight that start at
@@ -144,7 +152,7 @@ struct Part {
   Slot* table;
   int32_t slots;
   bool sparse;  // some bit may be clear (other than outside the part)
-  float inv;
+  float k;
 
   __device__ __forceinline__ void start(const LogitArgs& A, int64_t row, int32_t part, int32_t parts, int32_t n_slots, uint32_t* shared) {
     const int32_t per = (A.classes + parts - 1) / parts;
@@ -154,7 +162,7 @@ struct Part {
     first = lo - static_cast<int32_t>((reinterpret_cast<uintptr_t>(src + lo) & 15) / sizeof(T));
     chunks = (hi - first + 7) >> 3;
     const Rules rules(A.r);
-    inv = rules.inv_temperature;
+    k = kLog2e / A.r.temperature;
     slots = n_slots;
     const uint32_t* mask = mask_of(A, row);
     sparse = mask || slots;
@@ -188,9 +196,9 @@ struct Part {
       const int32_t at = s.id - first;
       if (shared[at >> 5] >> (at & 31) & 1u) {
         atomicAnd(&shared[at >> 5], ~(1u << (at & 31)));
-        s.z = rules(as_float(src[s.id]), s.count, s.bias ? A.r.bias_values[list + s.bias - 1] : 0.0f);
+        s.x = rules(as_float(src[s.id]), s.count, s.bias ? A.r.bias_values[list + s.bias - 1] : 0.0f);
       } else {
-        s.z = -__builtin_inff();  // masked
+        s.x = -__builtin_inff();  // masked
       }
     }
     __syncthreads();
@@ -209,90 +217,109 @@ struct Part {
   }
 
   // the logits of chunk c, -infinity where its bits are clear; false: the chunk is cut short
-  __device__ __forceinline__ bool load(int32_t c, float (&z)[8]) const {
+  __device__ __forceinline__ bool load(int32_t c, float (&x)[8]) const {
     const int32_t w = first + 8 * c;
     const bool whole = w >= lo && w + 8 <= hi;
     if (whole) {
-      load8(src + w, z);
+      load8(src + w, x);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = w + i >= lo && w + i < hi ? as_float(src[w + i]) : -__builtin_inff();
+      for (int i = 0; i < 8; ++i) x[i] = w + i >= lo && w + i < hi ? as_float(src[w + i]) : -__builtin_inff();
     }
-    const uint32_t bits = sparse ? open[c] : 255u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = bits >> i & 1u ? z[i] * inv : -__builtin_inff();
+    if (sparse) mask(x, open[c]);
     return whole;
   }
-
-  __device__ __forceinline__ Sum sum(int32_t target, float* zt) const {
-    Sum s{-__builtin_inff(), 0.0f};
-    for (int32_t c = threadIdx.x; c < chunks; c += 256) {
-      float z[8];
-      load(c, z);
-      add(s, z);
-      const uint32_t t = static_cast<uint32_t>(target - (first + 8 * c));
-      if (t < 8) {
+  static __device__ __forceinline__ void mask(float (&x)[8], uint32_t bits) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (t == i && z[i] != -__builtin_inff()) *zt = z[i];
-      }
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t keep = static_cast<uint32_t>(static_cast<int32_t>(bits << (31 - i)) >> 31);  // all ones where the bit is set
+      x[i] = __uint_as_float((__float_as_uint(x[i]) & keep) | (0xFF800000u & ~keep));
     }
+  }
+
+  __device__ __forceinline__ Sum sum(int32_t target, float* xt) const {
+    Sum s{-__builtin_inff(), 0.0f};
+    // whole chunks, two at a time: two loads on their way, and one rescaling for both
+    int32_t c = threadIdx.x;
+    const int32_t last = (hi - first) >> 3;  // chunks that end inside
+    if (c == 0 && first < lo && c < chunks) one(s, c), c += 256;
+    for (; c + 256 < last; c += 512) {
+      float x[16];
+      load8(src + first + 8 * c, *reinterpret_cast<float(*)[8]>(x));
+      load8(src + first + 8 * (c + 256), *reinterpret_cast<float(*)[8]>(x + 8));
+      if (sparse) {
+        mask(*reinterpret_cast<float(*)[8]>(x), open[c]);
+        mask(*reinterpret_cast<float(*)[8]>(x + 8), open[c + 256]);
+      }
+      add(s, x, k);
+    }
+    for (; c < chunks; c += 256) one(s, c);
     for (int32_t i = threadIdx.x; i < slots; i += 256) {
       if (table[i].id < 0) continue;
-      const float z[1] = {table[i].z};
-      add(s, z);
-      if (table[i].id == target) *zt = z[0];
+      const float x[1] = {table[i].x};
+      add(s, x, k);
+      if (table[i].id == target) *xt = x[0];
+    }
+    // the target, if it is neither masked nor named
+    if (threadIdx.x == 0 && target >= lo && target < hi) {
+      const int32_t at = target - first;
+      if (!sparse || open[at >> 3] >> (at & 7) & 1) *xt = as_float(src[target]);
     }
     return s;
+  }
+  __device__ __forceinline__ void one(Sum& s, int32_t c) const {
+    float x[8];
+    load(c, x);
+    add(s, x, k);
   }
 
   __device__ __forceinline__ void write(float* dst, Lse lse) const {
     const bool even = ((reinterpret_cast<uintptr_t>(dst + first) & 15) == 0);
     for (int32_t c = threadIdx.x; c < chunks; c += 256) {
-      float z[8];
-      const bool whole = load(c, z);
+      float x[8];
+      const bool whole = load(c, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = log_prob(z[i], lse);
+      for (int i = 0; i < 8; ++i) x[i] = log_prob(x[i], k, lse);
       const int32_t w = first + 8 * c;
       if (whole && even) {
-        store8(dst + w, z);
+        store8(dst + w, x);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (w + i >= lo && w + i < hi) dst[w + i] = z[i];
+          if (w + i >= lo && w + i < hi) dst[w + i] = x[i];
       }
     }
     if (!slots) return;
     __syncthreads();  // the named classes' places have been written above, as masked
     for (int32_t i = threadIdx.x; i < slots; i += 256)
-      if (table[i].id >= 0) dst[table[i].id] = log_prob(table[i].z, lse);
+      if (table[i].id >= 0) dst[table[i].id] = log_prob(table[i].x, k, lse);
   }
 };
 
 // One part of a row: its sum, and all the rest where the row has one part.  The
-// parts' sums are kept at part[row][split] = (m, l), the target's z after them.
+// parts' sums are kept at part[row][split] = (m, l), the target's logit after them.
 template <typename T>
 __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
-  __shared__ float zt;
+  __shared__ float xt;
   const int64_t row = A.row0 + blockIdx.x / A.splits;
   const int32_t part = static_cast<int32_t>(blockIdx.x % A.splits);
   Part<T> P;
-  if (threadIdx.x == 0) zt = -__builtin_inff();
+  if (threadIdx.x == 0) xt = -__builtin_inff();
   P.start(A, row, part, A.splits, slots, shared);
   const int32_t target = A.score ? A.target[row] : -1;
-  if (!P.sparse) __syncthreads();  // zt
-  Sum s = block_sum(P.sum(target, &zt));  // its barrier also shows zt to all
+  if (!P.sparse) __syncthreads();  // xt
+  Sum s = block_sum(P.sum(target, &xt), P.k);  // its barrier also shows xt to all
   if (A.splits > 1) {
     if (threadIdx.x == 0) {
       A.part[2 * (row * A.splits + part)] = s.m;
       A.part[2 * (row * A.splits + part) + 1] = s.l;
-      if (target >= P.lo && target < P.hi) A.part[2 * A.rows * A.splits + row] = zt;
+      if (target >= P.lo && target < P.hi) A.part[2 * A.rows * A.splits + row] = xt;
     }
     return;
   }
   const Lse lse = log_sum(s);
-  if (threadIdx.x == 0) finish(A, row, lse, zt);
+  if (threadIdx.x == 0) finish(A, row, lse, xt, P.k);
   if (A.logprobs) P.write(A.logprobs + row * A.out_stride, lse);
 }
 
@@ -304,10 +331,11 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitArgs A, int32_t slots)
   const int64_t row = A.row0 + blockIdx.x / parts;
   const int32_t part = static_cast<int32_t>(blockIdx.x % parts);
   Sum s{-__builtin_inff(), 0.0f};
-  for (int32_t k = threadIdx.x; k < A.splits; k += 256) join(s, A.part[2 * (row * A.splits + k)], A.part[2 * (row * A.splits + k) + 1]);
-  s = block_sum(s);
+  const float k = kLog2e / A.r.temperature;
+  for (int32_t i = threadIdx.x; i < A.splits; i += 256) join(s, A.part[2 * (row * A.splits + i)], A.part[2 * (row * A.splits + i) + 1], k);
+  s = block_sum(s, k);
   const Lse lse = log_sum(s);
-  if (part == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row]);
+  if (part == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row], k);
   if (!A.logprobs) return;
   Part<T> P;
   P.start(A, row, part, A.splits, slots, shared);
@@ -343,16 +371,21 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
     for (int e = 0; e < E; ++e)
       if (const int32_t p = place[at][lane + L * e]) bias[e] = A.r.bias_values[p - 1];
   }
+  const float k = kLog2e / A.r.temperature;
+  float next[E];  // the row that follows, on its way
+  const auto fetch = [&](int64_t row) {
+    const T* src = static_cast<const T*>(A.logits) + row * A.stride;
+#pragma unroll
+    for (int e = 0; e < E; ++e) next[e] = row < A.rows && lane + L * e < A.classes ? as_float(src[lane + L * e]) : -__builtin_inff();
+  };
+  fetch(static_cast<int64_t>(blockIdx.x) * rows + at);
   for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * rows; r0 < A.rows; r0 += static_cast<int64_t>(gridDim.x) * rows) {
     const int64_t row = r0 + at;
     const bool live = row < A.rows;
-    float z[E];
-    const T* src = static_cast<const T*>(A.logits) + row * A.stride;
+    float x[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int32_t w = lane + L * e;
-      z[e] = live && w < A.classes ? as_float(src[w]) : -__builtin_inff();
-    }
+    for (int e = 0; e < E; ++e) x[e] = next[e];
+    fetch(row + static_cast<int64_t>(gridDim.x) * rows);
     int32_t n[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) n[e] = 0;
@@ -385,31 +418,30 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int32_t w = lane + L * e;
-      z[e] = rules(z[e], n[e], bias[e]);
-      if (w >= A.classes || (mask && !(mask[w >> 5] >> (w & 31) & 1u))) z[e] = -__builtin_inff();
-      m = fmaxf(m, z[e]);
+      x[e] = rules(x[e], n[e], bias[e]);
+      if (w >= A.classes || (mask && !(mask[w >> 5] >> (w & 31) & 1u))) x[e] = -__builtin_inff();
+      m = fmaxf(m, x[e]);
     }
-    m = over_lanes<L>(m, Max());
-    Sum s{m, 0.0f};
-    const float base = safe(m);
+    Sum s{over_lanes<L>(m, Max()), 0.0f};
+    const float base = safe(s.m);
 #pragma unroll
-    for (int e = 0; e < E; ++e) s.l += exp_of(z[e], base);
+    for (int e = 0; e < E; ++e) s.l += term(x[e], base, k);
     s.l = over_lanes<L>(s.l, Plus());
     const Lse lse = log_sum(s);
     if (!live) continue;
-    if (A.lse && lane == 0) A.lse[row] = lse.m + lse.rest;
+    if (A.lse && lane == 0) A.lse[row] = lse.value(A.r.temperature);
     if (A.score) {
       const int32_t t = A.target[row];
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (lane + L * e == t && t < A.classes) A.score[row] = log_prob(z[e], lse);
+        if (lane + L * e == t && t < A.classes) A.score[row] = log_prob(x[e], k, lse);
       if (lane == 0 && (t < 0 || t >= A.classes)) A.score[row] = t < 0 ? 0.0f : __builtin_nanf("");
     }
     if (A.logprobs) {
       float* dst = A.logprobs + row * A.out_stride;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (lane + L * e < A.classes) dst[lane + L * e] = log_prob(z[e], lse);
+        if (lane + L * e < A.classes) dst[lane + L * e] = log_prob(x[e], k, lse);
     }
   }
 }
@@ -417,8 +449,8 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
 template <typename T, int L, int E>
 hipError_t run_short(const LogitArgs& A, hipStream_t st) {
   const int64_t groups = (A.rows + 256 / L - 1) / (256 / L);
-  // eight workgroups a CU are resident; more than a few times that only repeats the shared bias list's setup
-  k_logits_short<T, L, E><<<dim3(static_cast<unsigned>(groups < 4096 ? groups : 4096)), 256, 0, st>>>(A);
+  // as many workgroups as are resident: each has the next rows on their way while it works on its own
+  k_logits_short<T, L, E><<<dim3(static_cast<unsigned>(groups < 2048 ? groups : 2048)), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 

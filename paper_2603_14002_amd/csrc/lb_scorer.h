@@ -49,7 +49,7 @@ struct AttendArgs {
   // the plan's
   int32_t tiles, splits, part_rows;
   int64_t units, part_sums;
-  bool few;
+  bool few, alone;
 };
 
 struct LoraArgs {
@@ -75,11 +75,11 @@ struct LogitArgs {
 };
 
 // How an attention call is cut up (see attend_plan).  Few-row kernel: `few`, tiles
-// of 16 query rows a sequence and KV head, the parts that a key range is cut into,
+// of 16 query rows a sequence and KV head, whether a wavefront takes one alone, the parts that a key range is cut into,
 // the rows of a tile whose parts are kept, the floats of these and where the parts'
 // sums start among them.  Many-row kernel: its units of rows, 0: none.
 struct AttendPlan {
-  bool few;
+  bool few, alone;
   int32_t tiles, splits, part_rows;
   int64_t part_floats, part_sums, units;
 };

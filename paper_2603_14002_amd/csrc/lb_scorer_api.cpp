@@ -245,6 +245,7 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     A.units = p.units;
     A.part_sums = p.part_sums;
     A.few = p.few;
+    A.alone = p.alone;
     return launch_kv_attend(A, cache->head_dim, dtype, static_cast<hipStream_t>(stream));
   });
 }
