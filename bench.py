@@ -1,6 +1,6 @@
 """Throughput of the MI355X LightBeam decoding path on one GPU.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload c4] [--fusion-scorer lm] [--merge max]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--workload c4] [--fusion-scorer lm|lm-cached] [--merge max]
 
 One step decodes one whole batch of the workload (LB_BEGIN | LB_END over all
 frames; streaming workloads are fed chunk by chunk) with the inputs already in
@@ -50,7 +50,7 @@ def parse():
                     help="max: paths into one prefix recombined by their maximum (the best alignment, App. E.1) "
                          "instead of log-sum-exp; the committed traffic and parity figures are for log-sum-exp, "
                          "so the line reports them as null")
-    ap.add_argument("--fusion-scorer", choices=("synthetic", "lm"), default="synthetic",
+    ap.add_argument("--fusion-scorer", choices=("synthetic", "lm", "lm-cached"), default="synthetic",
                     help="lm: fusion scores come back through the external round trip from a small "
                          "randomly initialised causal word LM (the LLM stand-in)")
     ap.add_argument("--gather-ceiling", type=float, default=0.0, metavar="GB",
@@ -288,7 +288,7 @@ def main():
     B, T = d.logits.shape[:2]
     log(f"workload {wl.name}: B={B} T={T} K={p.beam} lm={d.lm.counts} ({time.time() - t0:.1f}s)")
     t0 = time.time()
-    external = args.fusion_scorer == "lm"
+    external = args.fusion_scorer != "synthetic"
     if external and p.fusion_interval <= 0:
         raise SystemExit(f"workload {wl.name} has no fusion")
     lp = lbm.make_params(p, max_batch=B, max_frames=T, fusion_seed=d.fusion_seed,
@@ -317,8 +317,11 @@ def main():
 
     rt = None
     if external:
-        from workloads.fusion_lm import CausalWordLM, RoundTripStats, decode_external
+        from workloads.fusion_lm import CachedWordLM, CausalWordLM, RoundTripStats, decode_external
         flm = CausalWordLM(d.lm.vocab_size, d.lm.bos, seed=d.fusion_seed & 0xFFFFFFFF).to(dev)
+        if args.fusion_scorer == "lm-cached":
+            flm = CachedWordLM(flm, n_pages=1 << 18)
+        rt_batch = 256 if args.fusion_scorer == "lm" else 4096  # ragged batches have no padding to keep small
         fwords = torch.empty((B, K, lp.subbeams, W), dtype=torch.int32, device=dev)
         fnw = torch.empty((B, K, lp.subbeams), dtype=torch.int32, device=dev)
         rt = RoundTripStats()
@@ -326,8 +329,10 @@ def main():
     def step():
         for lg, ln, tc, fl in chunks:
             if external:
+                if args.fusion_scorer == "lm-cached" and fl & lbm.LB_BEGIN:
+                    flm.reset()  # a batch's first call finds nothing of the batch before
                 decode_external(lbm, dec, lg, ln, fl, flm.score, hyps, scores, fwords, fnw, stream=stream,
-                                stats=rt)
+                                batch=rt_batch, stats=rt)
                 continue
             st = lbm.lb_decode_batch(dec.handle, lg, ln, B, tc, fl, stream, hyps, scores)
             assert st == lbm.LB_OK
@@ -460,7 +465,8 @@ def main():
     if external:
         n = args.steps
         out["config"]["fusion_scorer"] = ("external round trip: causal word LM (d=256, 2 layers, 4 heads, "
-                                          "random init, fp32), distinct sequences in batches of 256")
+                                          f"random init, fp32), distinct sequences in batches of {rt_batch}"
+                                          + (", over a paged 4-bit cache" if args.fusion_scorer == "lm-cached" else ""))
         out["round_trip"] = {
             "events_per_step": rt_clean["events"] / n,
             "sequences_requested_per_step": rt_clean["requested"] / n,

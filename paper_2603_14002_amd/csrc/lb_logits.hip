@@ -23,9 +23,13 @@ __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__bf16 x) { return static_cast<float>(x); }
 __device__ __forceinline__ float as_float(_Float16 x) { return static_cast<float>(x); }
 
+// the mask of a row where there are masks; none if outside 0 .. mask_rows - 1
+__device__ __forceinline__ int64_t mask_index(const LogitArgs& A, int64_t row) {
+  return A.r.mask_row ? A.r.mask_row[row] : A.r.mask_rows == 1 ? 0 : row;
+}
 __device__ __forceinline__ const uint32_t* mask_of(const LogitArgs& A, int64_t row) {
   if (!A.r.mask) return nullptr;
-  const int64_t k = A.r.mask_row ? A.r.mask_row[row] : A.r.mask_rows == 1 ? 0 : row;
+  const int64_t k = mask_index(A, row);
   return k >= 0 && k < A.r.mask_rows ? A.r.mask + k * ((A.classes + 31) / 32) : nullptr;
 }
 
@@ -372,20 +376,37 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
       if (const int32_t p = place[at][lane + L * e]) bias[e] = A.r.bias_values[p - 1];
   }
   const float k = kLog2e / A.r.temperature;
-  float next[E];  // the row that follows, on its way
+  const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
+  // on their way: the row that follows, its mask, and the number of the mask of the row after it
+  float next[E];
+  uint32_t next_mask[E];
+  int64_t mask_id = -1;
+  const auto fetch_id = [&](int64_t row) {
+    if (A.r.mask && row < A.rows) mask_id = mask_index(A, row);
+  };
   const auto fetch = [&](int64_t row) {
     const T* src = static_cast<const T*>(A.logits) + row * A.stride;
+    const bool masked = mask_id >= 0 && mask_id < A.r.mask_rows;
+    const uint32_t* mask = A.r.mask + (masked ? mask_id * ((A.classes + 31) / 32) : 0);
 #pragma unroll
-    for (int e = 0; e < E; ++e) next[e] = row < A.rows && lane + L * e < A.classes ? as_float(src[lane + L * e]) : -__builtin_inff();
+    for (int e = 0; e < E; ++e) {
+      const int32_t w = lane + L * e;
+      const bool there = row < A.rows && w < A.classes;
+      next[e] = there ? as_float(src[w]) : -__builtin_inff();
+      next_mask[e] = there && masked ? mask[w >> 5] : 0xFFFFFFFFu;
+    }
+    fetch_id(row + step);
   };
+  fetch_id(static_cast<int64_t>(blockIdx.x) * rows + at);
   fetch(static_cast<int64_t>(blockIdx.x) * rows + at);
-  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * rows; r0 < A.rows; r0 += static_cast<int64_t>(gridDim.x) * rows) {
+  for (int64_t r0 = static_cast<int64_t>(blockIdx.x) * rows; r0 < A.rows; r0 += step) {
     const int64_t row = r0 + at;
     const bool live = row < A.rows;
     float x[E];
+    uint32_t mask[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = next[e];
-    fetch(row + static_cast<int64_t>(gridDim.x) * rows);
+    for (int e = 0; e < E; ++e) x[e] = next[e], mask[e] = next_mask[e];
+    fetch(row + step);
     int32_t n[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) n[e] = 0;
@@ -413,13 +434,12 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
       }
       __syncthreads();
     }
-    const uint32_t* mask = live ? mask_of(A, row) : nullptr;
     float m = -__builtin_inff();
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int32_t w = lane + L * e;
       x[e] = rules(x[e], n[e], bias[e]);
-      if (w >= A.classes || (mask && !(mask[w >> 5] >> (w & 31) & 1u))) x[e] = -__builtin_inff();
+      if (w >= A.classes || !(mask[e] >> (w & 31) & 1u)) x[e] = -__builtin_inff();
       m = fmaxf(m, x[e]);
     }
     Sum s{over_lanes<L>(m, Max()), 0.0f};

@@ -69,10 +69,11 @@ __global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
   constexpr int W = kDownWaves<RT>, U = RT <= 2 ? 4 : 2, KS = 2 * S::KS;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
+  const int32_t r0 = static_cast<int32_t>(blockIdx.z) * (16 * RT);  // the first of the workgroup's entries of the rank
   __shared__ float red[W][RT * 4][64];
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   each_adapter(adapter_of(A, row), blockIdx.y, gridDim.y, [&](int32_t a, bool mine) {
-    const T* w = static_cast<const T*>(A.a) + static_cast<int64_t>(a) * A.rank * A.d_in + static_cast<int64_t>(n) * A.d_in;
+    const T* w = static_cast<const T*>(A.a) + (static_cast<int64_t>(a) * A.rank + r0 + n) * A.d_in;
     f32x4 acc[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) acc[r] = f32x4{0, 0, 0, 0};
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
             wf[u][v][r] = typename S::V{};
-            if (r * 16 + n < A.rank && k < A.d_in)
+            if (r0 + r * 16 + n < A.rank && k < A.d_in)
               wf[u][v][r] = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(r * 16) * A.d_in + k);
           }
         }
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
       float sum = 0.0f;
 #pragma unroll
       for (int k = 0; k < W; ++k) sum += red[k][at][lane];
-      const int k = (at >> 2) * 16 + 4 * j + (at & 3);
+      const int k = r0 + (at >> 2) * 16 + 4 * j + (at & 3);
       if (mine && k < A.rank) A.h[row * A.rank + k] = sum;
     }
   });
@@ -194,24 +195,47 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
   const uint32_t chunks = (A.d_out + kUpChannels - 1) / kUpChannels;  // side by side: rows are streamed
   const int64_t row = static_cast<int64_t>(blockIdx.x / chunks) * 16 + n;
   const int32_t o_lo = blockIdx.x % chunks * kUpChannels + wave * (kUpChannels / 4);
-  // a lane has the channels o_lo + 8 G j .. + 8 G - 1 of its row: rows are read and written in whole lines
-  const int32_t own = o_lo + 8 * G * j;
-  const T* src = static_cast<const T*>(A.y) + row * A.y_stride + own;
-  T* dst = static_cast<T*>(A.out) + row * A.out_stride + own;
+  // A lane has the channels o_lo + 32 g + 8 j .. + 7 of its row (32 bits: 4 j .. + 3
+  // of both 16): the four lanes of a row read and write 64 adjacent bytes at a time.
+  const T* src = static_cast<const T*>(A.y) + row * A.y_stride;
+  T* dst = static_cast<T*>(A.out) + row * A.out_stride;
+  const auto load = [&](float (&y)[8], int g) {
+    const int32_t o = o_lo + 32 * g;
+    if constexpr (H::wide) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x4 v{0, 0, 0, 0};
+        if (o + 16 * u + 4 * j < A.d_out) v = *reinterpret_cast<const f32x4*>(src + o + 16 * u + 4 * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[4 * u + i] = v[i];
+      }
+    } else if (o + 8 * j < A.d_out) {
+      load8(src + o + 8 * j, y);
+    }
+  };
+  const auto store = [&](const float (&y)[8], int g) {
+    const int32_t o = o_lo + 32 * g;
+    if constexpr (H::wide) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (o + 16 * u + 4 * j < A.d_out)
+          *reinterpret_cast<f32x4*>(dst + o + 16 * u + 4 * j) = f32x4{y[4 * u], y[4 * u + 1], y[4 * u + 2], y[4 * u + 3]};
+    } else if (o + 8 * j < A.d_out) {
+      store8(dst + o + 8 * j, y);
+    }
+  };
   float y[G][8];
   const bool early = gridDim.y == 1 && row < A.rows;  // else the tile's other workgroups would read the row too
   if (early)
 #pragma unroll
-    for (int g = 0; g < G; ++g)
-      if (own + 8 * g < A.d_out) load8(src + 8 * g, y[g]);
+    for (int g = 0; g < G; ++g) load(y[g], g);
   const int32_t id = adapter_of(A, row);
   if (blockIdx.y == 0 && id < 0 && row < A.rows && A.out != A.y)
 #pragma unroll
-    for (int g = 0; g < G; ++g)
-      if (own + 8 * g < A.d_out) {
-        if (!early) load8(src + 8 * g, y[g]);
-        store8(dst + 8 * g, y[g]);
-      }
+    for (int g = 0; g < G; ++g) {
+      if (!early) load(y[g], g);
+      store(y[g], g);
+    }
   each_adapter(id, blockIdx.y, gridDim.y, [&](int32_t a, bool mine) {
     // everything that the lane reads is on its way before the first product
     const T* w = static_cast<const T*>(A.b) + static_cast<int64_t>(a) * A.d_out * A.rank;
@@ -220,8 +244,8 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
     for (int g = 0; g < G; ++g)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        // row m of the operand is channel 8 G (m / 4) + 8 g + 4 u + m % 4: a lane gets 8 G adjacent ones
-        const int32_t o = o_lo + (n >> 2) * 8 * G + g * 8 + u * 4 + (n & 3);
+        // the channel of row m of the operand: the lane of results 4 j .. 4 j + 3 gets those that are its own
+        const int32_t o = o_lo + g * 32 + (H::wide ? u * 16 + n : (n >> 2) * 8 + u * 4 + (n & 3));
 #pragma unroll
         for (int c = 0; c < H::N; ++c) {
           const int32_t k = H::entry(c, j, A.rank);
@@ -231,8 +255,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
       }
     if (!early && mine)
 #pragma unroll
-      for (int g = 0; g < G; ++g)
-        if (own + 8 * g < A.d_out) load8(src + 8 * g, y[g]);
+      for (int g = 0; g < G; ++g) load(y[g], g);
     H h;
     h.load(A, row, mine, j);
     const float scale = (A.scale ? A.scale[a] : 1.0f) * h.unit;
@@ -247,14 +270,14 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
 #pragma unroll
           for (int p = 0; p < H::pieces; ++p) acc[u] = S::mul(wf[g][u][c], h.v[p][c], acc[u]);
       }
-      if (mine && own + 8 * g < A.d_out) {
+      if (mine) {
         float z[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           z[i] = fmaf(scale, acc[0][i], y[g][i]);
           z[4 + i] = fmaf(scale, acc[1][i], y[g][4 + i]);
         }
-        store8(dst + 8 * g, z);
+        store(z, g);
       }
     }
   });
@@ -266,7 +289,11 @@ hipError_t run(const LoraArgs& A, hipStream_t st) {
   const unsigned chunks = static_cast<unsigned>((A.d_out + kUpChannels - 1) / kUpChannels);
   // few tiles: the adapters of a tile side by side
   const unsigned down = tiles < 512 ? 16 : 1, up = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
-  k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves<RT>, 0, st>>>(A);
+  // and the rank's tiles too, each with its part of the weights (RANK_FIGURES)
+  if (RT > 1 && tiles < 64)
+    k_lora_down<T, 1><<<dim3(tiles, down, (A.rank + 15) / 16), 64 * kDownWaves<1>, 0, st>>>(A);
+  else
+    k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves<RT>, 0, st>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   k_lora_up<T, RT><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);

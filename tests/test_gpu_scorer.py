@@ -705,3 +705,108 @@ def test_new_memory_belongs_to_the_call_s_stream():
     null = lbm.lb_logits_adjust(logits, target=target, stream=0)
     torch.cuda.synchronize()
     assert torch.equal(null[2], new[2])
+
+
+# ------------------------------------------------------------------ the cached word LM
+
+
+def lm64(lm, cached, key, adapters=None):
+    """The model in 64 bits on the keys and values that the cache holds of a sequence: its score, and how far these
+    are from the model's own, as a part of their block's largest."""
+    which, words = key
+    n, hd = len(words), lm.d // lm.h
+    pages = cached.held[key][0]
+    R = ref.Ragged([], [], cached.P, lm.h, hd)
+    R.table = torch.tensor([pages], dtype=torch.int32)
+    norm = lambda x: (x - x.mean(-1, keepdim=True)) / torch.sqrt(x.var(-1, keepdim=True, unbiased=False) + 1e-5)
+    W = lambda p: p.detach().cpu().double()
+    z = W(lm.emb)[[lm.bos] + list(words[:-1])] + W(lm.pos)[:n]
+    off = 0.0
+    for i, m in enumerate(lm.layers):
+        k, v = R.get(0, n, cached.caches[i].pages.cpu())
+        a = norm(z)
+        qkv = a @ W(m.qkv).t()
+        if adapters is not None and 0 <= which < adapters[i][0].shape[0]:
+            qkv = qkv + a @ W(adapters[i][0][which]).t() @ W(adapters[i][1][which]).t()
+        q, kk, vv = (x.reshape(n, lm.h, hd) for x in qkv.split(lm.d, dim=1))
+        for got, own in ((k, kk), (v, vv)):
+            most = own.unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True)
+            off = max(off, float(((got - own).unflatten(-1, (-1, 32)).abs() / most).max()))
+        o = ref.attend(q, k, v, 1 / math.sqrt(hd), 0, 0)[0]
+        z = z + o.reshape(n, lm.d) @ W(m.proj).t()
+        h = norm(z) @ W(m.up).t()
+        z = z + (h * 0.5 * (1 + torch.erf(h / math.sqrt(2)))) @ W(m.down).t()
+    lp = torch.log_softmax(norm(z) @ W(lm.emb).t() * lm.out_scale, 1)
+    return float(lp[torch.arange(n), list(words)].sum()), off
+
+
+def test_cached_lm_scores():
+    """Sequences that grow over several calls, branch inside a page, repeat and come back after they made room: each
+    score is the 64-bit one on the cache's contents, whose keys and values are the model's to half a step of 4 bits."""
+    from workloads.fusion_lm import CachedWordLM, CausalWordLM
+    V, BOS, d = 600, 599, 128
+    lm = CausalWordLM(V, BOS, d_model=d, n_layers=2, n_heads=2, max_len=64, seed=5).to("cuda:0")
+    g = torch.Generator().manual_seed(3)
+    adapters = [(torch.randn(3, 8, d, generator=g).to("cuda:0") * 0.05, torch.randn(3, 3 * d, 8, generator=g).to("cuda:0") * 0.05)
+                for _ in range(2)]
+    rng = np.random.default_rng(4)
+    word = lambda n: [int(x) for x in rng.integers(0, V, n)]
+    a, b = word(13), word(30)
+    calls = [[a[:5], b, [], a[:5]],
+             [a, a[:5] + word(14), b + word(9), b[:16] + word(3), a[:5] + word(1)],
+             [a + word(20), a, word(1), b],
+             [word(40), word(47), word(33), word(50), word(44), word(61), word(17)],
+             [a[:5] + word(2), b]]
+    for use in (None, adapters):
+        cached = CachedWordLM(lm, n_pages=26, adapters=use)
+        for k, seqs in enumerate(calls):
+            say(f"[case] cached lm {use is not None} call {k}")
+            L = max(1, max(map(len, seqs)))
+            rows = torch.full((len(seqs), L), -1, dtype=torch.int32)
+            for i, s in enumerate(seqs):
+                rows[i, :len(s)] = torch.tensor(s, dtype=torch.int32)
+            lens = torch.tensor([len(s) for s in seqs])
+            ids = None if use is None else torch.tensor([(i % 4) - 1 for i in range(len(seqs))])
+            got = cached.score(rows.to("cuda:0"), lens.to("cuda:0"), ids)
+            assert [c.status() for c in cached.caches] == [0, 0]
+            for i, s in enumerate(seqs):
+                if not s:
+                    assert float(got[i]) == 0.0
+                    continue
+                want, off = lm64(lm, cached, (-1 if ids is None else int(ids[i]), tuple(s)), use)
+                # each word's log-probability: sums over d channels in 32 bits, through a dozen products and norms
+                assert abs(float(got[i]) - want) < len(s) * 64 * d * 2.0 ** -24
+                # half the widest step (4 to 6) is one scale, the scale less than a third of the largest value
+                assert off < (1 + 2.0 ** -10) / 3
+            in_use = sorted(p for pages, _ in cached.held.values() for p in set(pages))
+            assert all(cached.uses[p] == in_use.count(p) for p in range(26))
+            assert sorted(cached.free) == [p for p in range(26) if cached.uses[p] == 0]
+        before = dict(cached.held)
+        too_many = torch.randint(0, V, (8, 60), generator=g)
+        with pytest.raises(ValueError):
+            cached.score(too_many.to("cuda:0"), torch.full((8,), 60))
+        assert all(cached.uses[p] == sum(p in pages for pages, _ in cached.held.values()) for p in range(26))
+        assert set(cached.held) <= set(before)
+        with pytest.raises(ValueError):
+            cached.score(torch.zeros(1, 64, dtype=torch.int32), torch.tensor([64]))
+        cached.reset()
+        assert not cached.held and len(cached.free) == 26
+
+
+def test_cached_lm_answers_a_request():
+    """An exported request scored through the cached model: each asked sub-beam's score is the 64-bit one on the
+    cache's contents, the others get 0."""
+    from workloads.fusion_lm import CachedWordLM, CausalWordLM, score_requests
+    V, BOS, d = 200, 199, 256
+    lm = CausalWordLM(V, BOS, seed=2).to("cuda:0")
+    cached = CachedWordLM(lm, n_pages=512)
+    rng = np.random.default_rng(7)
+    words = torch.from_numpy(rng.integers(0, V, (2, 4, 2, 16)).astype(np.int32))
+    for n in (3, 6, 11):  # the same words, more of them each time
+        counts = torch.from_numpy(rng.integers(-1, n + 1, (2, 4, 2)).astype(np.int32))
+        say(f"[case] request {n}")
+        got = score_requests(words.to("cuda:0"), counts.to("cuda:0"), cached.score, batch=3).cpu()
+        for at in np.ndindex(*counts.shape):
+            m = int(counts[at])
+            want = lm64(lm, cached, (-1, tuple(words[at][:m].tolist())))[0] if m > 0 else 0.0
+            assert abs(float(got[at]) - want) <= max(m, 0) * 64 * d * 2.0 ** -24

@@ -15,11 +15,18 @@ the score array of ``lb_fusion_scores``, scoring each distinct sequence once.
 ``decode_external`` drives the whole round trip for one call of
 ``lb_decode_batch``.  All of this is caller code around the decoder's C ABI; the
 decoder computes nothing here.
+
+``CachedWordLM`` is the same model on the library's scorer operators
+(``include/lightbeam_scorer.h``): keys and values stay in a paged 4-bit cache, so
+a sequence that continues an earlier one costs its new words only, as most of a
+later fusion event's do, and batches are ragged, without padding.  Its scores are
+those of the model with keys and values rounded to 4 bits.
 """
 
 from __future__ import annotations
 
 import math
+from collections import OrderedDict
 from dataclasses import dataclass
 
 import torch
@@ -99,6 +106,145 @@ class CausalWordLM(torch.nn.Module):
             lp[s:s + token_chunk] = (logits.gather(1, tgt[s:s + token_chunk, None]).squeeze(1)
                                      - torch.logsumexp(logits, dim=1))
         return out.index_add_(0, row, lp)
+
+
+class CachedWordLM:
+    """Scores of a ``CausalWordLM`` over a paged 4-bit cache of keys and values.
+
+    The cache holds the sequences scored last, in pages of `page_tokens` tokens of
+    which `n_pages` exist for each layer; those not asked for longest make room.  A
+    sequence takes whole pages over from the longest of its prefixes there is, and a
+    copy of the one it goes on in.  All calls belong on one stream.  adapters: per layer (a [n, rank, d], b [n, 3 d,
+    rank]), low-rank corrections of the projection to queries, keys and values, one of
+    the n for each sequence of a call."""
+
+    def __init__(self, lm: CausalWordLM, n_pages: int = 4096, page_tokens: int = 16, adapters=None):
+        import paper_2603_14002_amd as lbm
+        self.lbm, self.lm, self.adapters, self.P = lbm, lm, adapters, page_tokens
+        dev = lm.emb.device
+        self.caches = [lbm.KVCache.empty(n_pages, page_tokens, lm.h, lm.d // lm.h, dev) for _ in lm.layers]
+        self.rules = lbm.LogitRules(temperature=1.0 / lm.out_scale)
+        self.free = list(range(n_pages))
+        self.uses = [0] * n_pages
+        self.held = OrderedDict()  # (adapter, words) -> (pages of positions 0..len(words)-1, score); the last used last
+
+    def reset(self) -> None:
+        """Forgets all sequences (the weights or the adapters have changed)."""
+        while self.held:
+            self._drop(next(reversed(self.held)))
+
+    def _drop(self, key) -> None:
+        for p in self.held.pop(key)[0]:
+            self._release(p)
+
+    def _release(self, page: int) -> None:
+        self.uses[page] -= 1
+        if self.uses[page] == 0:
+            self.free.append(page)
+
+    def _take(self, used) -> int:
+        """A free page; sequences outside `used` give way."""
+        while not self.free:
+            key = next((k for k in self.held if k not in used), None)
+            if key is None:
+                raise ValueError("the cache has too few pages for one batch of sequences")
+            self._drop(key)
+        page = self.free.pop()
+        self.uses[page] = 1
+        return page
+
+    @torch.no_grad()
+    def score(self, seqs: torch.Tensor, lengths: torch.Tensor, adapter=None) -> torch.Tensor:
+        """As ``CausalWordLM.score``; adapter: int [N] (outside 0..n-1: none), or None for none."""
+        dev, N = self.lm.emb.device, seqs.shape[0]
+        lens = lengths.tolist()
+        ids = [-1] * N if adapter is None else [int(a) for a in adapter]
+        keys = [(a, tuple(w[:n])) for a, w, n in zip(ids, seqs.tolist(), lens)]
+        for key in keys:
+            if len(key[1]) >= self.lm.max_len:
+                raise ValueError("a sequence is longer than the model's positions")
+        # what is there of every sequence: itself, or the longest prefix
+        used, new, copies = set(), [], []
+        for key in keys:
+            if key in used or not key[1]:
+                continue
+            prefix = next((k for k in ((key[0], key[1][:n]) for n in range(len(key[1]), 0, -1)) if k in self.held), None)
+            if prefix is not None:
+                self.held.move_to_end(prefix)
+                used.add(prefix)
+            if prefix != key:
+                new.append((key, prefix))
+            used.add(key)
+        done = []
+        try:
+            for key, prefix in new:
+                pages, score = self.held[prefix] if prefix else ([], 0.0)
+                there = len(prefix[1]) if prefix else 0
+                mine = []
+                done.append((key, mine, there, score))
+                for p in pages[:there // self.P]:
+                    self.uses[p] += 1
+                    mine.append(p)
+                for i in range(there // self.P, -(-len(key[1]) // self.P)):
+                    mine.append(self._take(used))
+                    if i * self.P < there:
+                        copies.append((pages[i], mine[-1]))
+            for (key, pages, _, old), got in zip(done, self._run(done, copies, dev) if done else ()):
+                self.held[key] = (pages, old + got)
+        except Exception:
+            for key, mine, _, _ in done:
+                for p in mine if key not in self.held else ():
+                    self._release(p)
+            raise
+        for key in keys:
+            if key in self.held:
+                self.held.move_to_end(key)
+        return torch.tensor([self.held[k][1] if k[1] else 0.0 for k in keys], dtype=torch.float32, device=dev)
+
+    def _run(self, todo, copies, dev):
+        """Appends what is new of the sequences and returns the sums of its log-probabilities."""
+        lbm, lm = self.lbm, self.lm
+        hd = lm.d // lm.h
+
+        def ints(x, dtype=torch.int32):
+            return torch.tensor(x, dtype=dtype, device=dev)
+
+        counts = [len(k[1]) - there for k, _, there, _ in todo]
+        width = max(len(pages) for _, pages, _, _ in todo)
+        starts, at = [0], []
+        for c, (_, _, there, _) in zip(counts, todo):
+            starts.append(starts[-1] + c)
+            at.extend(range(there, there + c))
+        rows = starts[-1]
+        batch = lbm.KVBatch(ints(starts), ints([len(k[1]) for k, _, _, _ in todo]),
+                            ints([p + [-1] * (width - len(p)) for _, p, _, _ in todo]), rows, max(counts))
+        # position i holds word i (position 0: <s>) and predicts word i + 1
+        tokens = ints([lm.bos if i == 0 else k[1][i - 1] for k, _, there, _ in todo for i in range(there, len(k[1]))], torch.int64)
+        targets = ints([w for k, _, there, _ in todo for w in k[1][there:]])
+        which = None
+        if self.adapters is not None:
+            which = ints([k[0] for (k, _, _, _), c in zip(todo, counts) for _ in range(c)])
+        if copies:
+            src, dst = ints([a for a, _ in copies], torch.int64), ints([b for _, b in copies], torch.int64)
+            for c in self.caches:
+                c.pages[dst] = c.pages[src]
+        z = lm.emb[tokens] + lm.pos[ints(at, torch.int64)]
+        for i, (m, cache) in enumerate(zip(lm.layers, self.caches)):
+            a = F.layer_norm(z, (lm.d,))
+            qkv = F.linear(a, m.qkv)
+            if which is not None:
+                lbm.lb_lora_add(qkv, a, *self.adapters[i], which)
+            q, k, v = (x.unflatten(1, (lm.h, hd)) for x in qkv.split(lm.d, dim=1))
+            lbm.lb_kv_append(cache, batch, None, k, v)
+            o, _ = lbm.lb_kv_attend(cache, batch, q, 1.0 / math.sqrt(hd))
+            z = z + F.linear(o.reshape(rows, lm.d), m.proj)
+            a = F.layer_norm(z, (lm.d,))
+            z = z + F.linear(F.gelu(F.linear(a, m.up)), m.down)
+        z = F.layer_norm(z, (lm.d,))
+        lp = torch.cat([lbm.lb_logits_adjust(F.linear(z[r:r + 4096], lm.emb), self.rules, target=targets[r:r + 4096],
+                                             want_logprobs=False)[1] for r in range(0, rows, 4096)])
+        row = torch.repeat_interleave(torch.arange(len(todo), device=dev), ints(counts, torch.int64), output_size=rows)
+        return torch.zeros(len(todo), dtype=torch.float64, device=dev).index_add_(0, row, lp.double()).tolist()
 
 
 @dataclass
