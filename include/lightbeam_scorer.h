@@ -45,8 +45,8 @@ enum { LB_F32 = 0, LB_BF16 = 1, LB_F16 = 2 };
 /* Keys and values in pages of page_tokens tokens.  Each block of 32 channels of
  * one head of one token holds 4-bit codes and a scale:
  *   value = code * 2^(scale - 127),  code in {0, 0.5, 1, 1.5, 2, 3, 4, 6} and
- *   their negatives (e2m1: bit 3 is the sign); scale 255 stands for NaN in the
- *   whole block.
+ *   their negatives (e2m1: bit 3 is the sign), scale in 3..252; scale 255 stands
+ *   for NaN in the whole block.
  * The memory of head h of page p starts at
  *   pages + (p * kv_heads + h) * page_tokens * (head_dim + head_dim / 16)
  * and holds, with P = page_tokens and D = head_dim,
@@ -84,11 +84,15 @@ typedef struct lb_kv_batch {
   const int32_t* starts;  /* device [n_seqs + 1], not decreasing, from 0 on     */
   const int32_t* lengths; /* device [n_seqs]: tokens with the new ones          */
   const int32_t* pages;   /* device [n_seqs][max_pages]                         */
-  int32_t n_seqs;
-  int32_t n_rows;         /* rows of the activations: at least starts[n_seqs]   */
+  int32_t n_seqs;         /* at most 2^22                                       */
+  int32_t n_rows;         /* rows of the activations: at least starts[n_seqs],
+                             at most 2^24                                       */
   int32_t max_pages;
   int32_t max_new;        /* at least every sequence's number of new tokens     */
 } lb_kv_batch;
+/* (max_pages * page_tokens is at most 2^30.  A call's workgroups number less than
+ * 2^24: lb_kv_attend refuses batches that need more, about 2^30 query rows and
+ * heads.) */
 
 /* Rotation of keys and queries: with row p of the tables for position p, the
  * pair (x1, x2) of channels becomes (x1 cos - x2 sin, x2 cos + x1 sin); pair i
@@ -128,10 +132,9 @@ lb_status lb_rope_table(int32_t positions, int32_t rot_dim, double base, int32_t
  * A block's scale is the smallest power of two 2^e, e in -124..125, with
  * |x| <= 6 * 2^e for its 32 values, each code the nearest (ties to the even code,
  * at most 6); keys are rotated in 64 bits first, so the codes are those of the
- * exact rotation.  A block with an infinity or a NaN gets scale 255.  Rows' strides are multiples of
- * 16 B and pointers 16-B aligned.  The sequences' slots must be distinct:
- * what two tokens of a call that share a slot leave there is one of the two,
- * block by block. */
+ * exact rotation.  A block with an infinity or a NaN gets scale 255.  Rows' strides
+ * are multiples of 16 B and pointers 16-B aligned.  The slots of a call's tokens
+ * must be distinct: what two tokens that share one leave there is not defined. */
 lb_status lb_kv_append(const lb_kv_cache* cache, const lb_kv_batch* batch, const lb_rope* rope, int32_t dtype,
                        int32_t q_heads, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                        const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride, void* stream);
@@ -170,6 +173,9 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
  *           row strides; out may be y itself with the same stride
  *   a, b    device [n_adapters][rank][d_in] and [n_adapters][d_out][rank]
  *   adapter device int32 [rows];  scale: device float32 [n_adapters], NULL: 1
+ *   workspace  device, 16-B aligned, at least what lb_lora_workspace says for
+ *              these rows and sizes (NULL if that is 0)
+ * rows at most 2^28, and rows / 16 * d_out / 256 below 2^24.
  * rank, d_in, d_out are multiples of 8, rank at most 128 (adapters of lower rank
  * are padded with zeros); strides are multiples of 16 B, pointers 16-B aligned. */
 lb_status lb_lora_workspace(int64_t rows, int32_t d_in, int32_t d_out, int32_t rank, int64_t* bytes);
@@ -190,8 +196,8 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
  * Ids outside 0..classes-1 in a history or a bias list are no entries; of several
  * biases for one class the last counts. */
 typedef struct lb_logit_rules {
-  float temperature;         /* > 0; 1: none                                    */
-  float repetition;          /* > 0; 1: none                                    */
+  float temperature;         /* a normal number > 0; 1: none                    */
+  float repetition;          /* a normal number > 0; 1: none                    */
   float presence, frequency; /* 0: none                                         */
   const int32_t* history;    /* device [rows][history_width] or NULL            */
   const int32_t* bias_ids;   /* device [rows or 1][bias_width] or NULL          */
@@ -217,6 +223,8 @@ enum { LB_MAX_RULE_IDS = 4096 };
  * -infinity whatever their logits hold, a row with nothing left -infinity
  * throughout.  rules NULL: none.
  *   logits    device [rows][classes] of `dtype`, row stride logits_stride
+ *   workspace  device, 16-B aligned, at least what lb_logits_workspace says for
+ *              these rows and classes (NULL if that is 0)
  * logits is only read; logprobs may be the logits themselves where these are
  * LB_F32 with the same stride. */
 lb_status lb_logits_workspace(int64_t rows, int32_t classes, int64_t* bytes);

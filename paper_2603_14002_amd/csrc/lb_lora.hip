@@ -1,8 +1,8 @@
 // Low-rank adapters beside a shared projection: out_i = y_i + s_a B_a (A_a x_i).
 //
 // Two launches: the rows' rank-sized products h = A x, kept in 32 bits, then out =
-// y + s B h.  Both work on 16 rows at a time and, within them, on the distinct adapters one after the other with the other adapters' rows
-// held at zero: rows of one request lie together, so a tile mostly has one
+// y + s B h (one for few rows and small weights).  Both work on 16 rows at a time
+// and, within them, on the distinct adapters with the other adapters' rows held at zero: rows of one request lie together, so a tile mostly has one
 // adapter, and where each row has its own the weights of every row's adapter
 // have to be read anyway.
 #include <hip/hip_runtime.h>
@@ -56,63 +56,75 @@ __device__ __forceinline__ int32_t adapter_of(const LoraArgs& A, int64_t row) {
   return a >= 0 && a < A.n_adapters ? a : -1;
 }
 
-// h[row][rank] for 16 rows: the wavefronts take every W-th piece of d_in and join
-// in LDS.  A piece is two matrix steps: a lane takes 32 adjacent bytes of its
-// row, so that the four lanes of a row read whole lines of 128 B.  U pieces are
-// on their way at a time.
-template <int RT>
+// A wavefront's share of h = A x for 16 rows and the rank's entries r0 .. r0 + 16 RT
+// - 1 (rows not `mine`: zero): every W-th piece of d_in.  A piece is two matrix
+// steps: a lane takes 32 adjacent bytes of its row, so that the four lanes of a row
+// read whole lines of 128 B.  U pieces are on their way at a time.
+template <typename T, int RT, int W>
+__device__ __forceinline__ void down_share(const LoraArgs& A, const T* x, int32_t a, int32_t r0, bool mine, int wave, int n, int j, f32x4 (&acc)[RT]) {
+  using S = Step<T>;
+  constexpr int U = RT <= 2 ? 4 : 2, KS = 2 * S::KS;
+  const T* w = static_cast<const T*>(A.a) + (static_cast<int64_t>(a) * A.rank + r0 + n) * A.d_in;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) acc[r] = f32x4{0, 0, 0, 0};
+  for (int32_t k0 = wave * KS; k0 < A.d_in; k0 += U * W * KS) {
+    typename S::V xf[U][2], wf[U][2][RT];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const int32_t k = k0 + u * W * KS + (2 * j + v) * S::W;
+        xf[u][v] = typename S::V{};
+        if (mine && k < A.d_in) xf[u][v] = *reinterpret_cast<const typename S::V*>(x + k);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          wf[u][v][r] = typename S::V{};
+          if (r0 + r * 16 + n < A.rank && k < A.d_in)
+            wf[u][v][r] = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(r * 16) * A.d_in + k);
+        }
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[r] = S::mul(wf[u][v][r], xf[u][v], acc[r]);
+  }
+}
+
+// Joins the wavefronts' shares in LDS: put(k, sum) for entry k of the lane's row.
+template <int RT, int W, typename F>
+__device__ __forceinline__ void down_join(float (&red)[W][RT * 4][64], const f32x4 (&acc)[RT], int wave, int lane, F&& put) {
+  __syncthreads();  // the last adapter's sums have been read
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[wave][4 * r + i][lane] = acc[r][i];
+  __syncthreads();
+  for (int at = wave; at < RT * 4; at += W) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) sum += red[k][at][lane];
+    put((at >> 2) * 16 + 4 * (lane >> 4) + (at & 3), sum);
+  }
+}
+
 constexpr int kDownWaves = 8;  // 64 KB of LDS at most
 
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * kDownWaves<RT>) void k_lora_down(LoraArgs A) {
-  using S = Step<T>;
-  constexpr int W = kDownWaves<RT>, U = RT <= 2 ? 4 : 2, KS = 2 * S::KS;
+__global__ __launch_bounds__(64 * kDownWaves) void k_lora_down(LoraArgs A) {
+  constexpr int W = kDownWaves;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 16 + n;
   const int32_t r0 = static_cast<int32_t>(blockIdx.z) * (16 * RT);  // the first of the workgroup's entries of the rank
   __shared__ float red[W][RT * 4][64];
   const T* x = static_cast<const T*>(A.x) + row * A.x_stride;
   each_adapter(adapter_of(A, row), blockIdx.y, gridDim.y, [&](int32_t a, bool mine) {
-    const T* w = static_cast<const T*>(A.a) + (static_cast<int64_t>(a) * A.rank + r0 + n) * A.d_in;
     f32x4 acc[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) acc[r] = f32x4{0, 0, 0, 0};
-    for (int32_t k0 = wave * KS; k0 < A.d_in; k0 += U * W * KS) {
-      typename S::V xf[U][2], wf[U][2][RT];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int32_t k = k0 + u * W * KS + (2 * j + v) * S::W;
-          xf[u][v] = typename S::V{};
-          if (mine && k < A.d_in) xf[u][v] = *reinterpret_cast<const typename S::V*>(x + k);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            wf[u][v][r] = typename S::V{};
-            if (r0 + r * 16 + n < A.rank && k < A.d_in)
-              wf[u][v][r] = *reinterpret_cast<const typename S::V*>(w + static_cast<int64_t>(r * 16) * A.d_in + k);
-          }
-        }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-          for (int r = 0; r < RT; ++r) acc[r] = S::mul(wf[u][v][r], xf[u][v], acc[r]);
-    }
-    __syncthreads();  // the last adapter's sums have been read
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) red[wave][4 * r + i][lane] = acc[r][i];
-    __syncthreads();
-    for (int at = wave; at < RT * 4; at += W) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) sum += red[k][at][lane];
-      const int k = r0 + (at >> 2) * 16 + 4 * j + (at & 3);
-      if (mine && k < A.rank) A.h[row * A.rank + k] = sum;
-    }
+    down_share<T, RT, W>(A, x, a, r0, mine, wave, n, j, acc);
+    down_join<RT, W>(red, acc, wave, lane, [&](int k, float sum) {
+      if (mine && r0 + k < A.rank) A.h[row * A.rank + r0 + k] = sum;
+    });
   });
 }
 
@@ -138,8 +150,7 @@ struct Down {
     return paired && q >= rank ? (q < 2 * rank ? q - rank : rank) : q;
   }
 
-  __device__ __forceinline__ void load(const LoraArgs& A, int64_t row, bool mine, int j) {
-    const float* h = A.h + row * A.rank;
+  __device__ __forceinline__ void load(const LoraArgs& A, const float* h, bool mine, int j) {
     unit = 1.0f;
     if constexpr (wide) {
 #pragma unroll
@@ -186,7 +197,9 @@ struct Down {
   }
 };
 
-template <typename T, int RT>
+// out = y + s B h.  whole: h is computed here too, by each workgroup for its own
+// channels, else k_lora_down has left it in the workspace.
+template <typename T, int RT, bool whole>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
   using S = Step<T>;
   using H = Down<T, RT>;
@@ -225,6 +238,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
     }
   };
   float y[G][8];
+  __shared__ float red[whole ? 4 : 1][RT * 4][64], own[whole ? 16 : 1][RT * 16 + 4];
   const bool early = gridDim.y == 1 && row < A.rows;  // else the tile's other workgroups would read the row too
   if (early)
 #pragma unroll
@@ -256,8 +270,16 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
     if (!early && mine)
 #pragma unroll
       for (int g = 0; g < G; ++g) load(y[g], g);
+    const float* from = A.h + row * A.rank;
+    if constexpr (whole) {
+      f32x4 acc[RT];
+      down_share<T, RT, 4>(A, static_cast<const T*>(A.x) + row * A.x_stride, a, 0, mine, wave, n, j, acc);
+      down_join<RT, 4>(red, acc, wave, lane, [&](int k, float sum) { own[n][k] = sum; });
+      __syncthreads();
+      from = own[n];
+    }
     H h;
-    h.load(A, row, mine, j);
+    h.load(A, from, mine, j);
     const float scale = (A.scale ? A.scale[a] : 1.0f) * h.unit;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -289,14 +311,20 @@ hipError_t run(const LoraArgs& A, hipStream_t st) {
   const unsigned chunks = static_cast<unsigned>((A.d_out + kUpChannels - 1) / kUpChannels);
   // few tiles: the adapters of a tile side by side
   const unsigned down = tiles < 512 ? 16 : 1, up = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
-  // and the rank's tiles too, each with its part of the weights (RANK_FIGURES)
-  if (RT > 1 && tiles < 64)
-    k_lora_down<T, 1><<<dim3(tiles, down, (A.rank + 15) / 16), 64 * kDownWaves<1>, 0, st>>>(A);
+  if constexpr (RT <= 2)
+    if (lora_whole(A.rows, A.d_in, A.d_out, A.rank)) {
+      k_lora_up<T, RT, true><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
+      return hipGetLastError();
+    }
+  // and with very few the rank's tiles too, each with its part of A, but x read again for each (rank 64, d_in 2048,
+  // bf16, d_out 512: 16 rows 9.6 us, else 15.3; 512 rows of their own adapters 34.7, else 30.4)
+  if (RT > 1 && tiles < 16)
+    k_lora_down<T, 1><<<dim3(tiles, down, (A.rank + 15) / 16), 64 * kDownWaves, 0, st>>>(A);
   else
-    k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves<RT>, 0, st>>>(A);
+    k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves, 0, st>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_lora_up<T, RT><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
+  k_lora_up<T, RT, false><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
   return hipGetLastError();
 }
 
@@ -306,6 +334,14 @@ hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
 }
 
 }  // namespace
+
+// Few rows and a small A: one launch, with h computed once for each 256 channels of
+// d_out.  8 rows of their own adapters, 256 -> 768, rank 16: 3.9 us in bf16 and 4.5 in
+// fp32, in two launches 6.0 and 6.9; 256 rows, 1024 -> 1024: 9.9 and 17, in two 9.2 and 11.
+bool lora_whole(int64_t rows, int32_t d_in, int32_t d_out, int32_t rank) {
+  return rows <= 256 && rank <= 32 && d_out <= 4 * kUpChannels && static_cast<int64_t>(d_in) * rank <= 16384 &&
+         rows * d_in * rank <= (1 << 20);
+}
 
 hipError_t launch_lora(const LoraArgs& A, int dtype, hipStream_t st) {
   return dtype == LB_F32 ? by_rank<float>(A, st) : dtype == LB_BF16 ? by_rank<__bf16>(A, st) : by_rank<_Float16>(A, st);

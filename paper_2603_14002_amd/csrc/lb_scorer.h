@@ -89,6 +89,8 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st);
 
+// the call is one launch, and needs no workspace
+bool lora_whole(int64_t rows, int32_t d_in, int32_t d_out, int32_t rank);
 hipError_t launch_lora(const LoraArgs& A, int dtype, hipStream_t st);
 
 // parts of a row that its sum is taken over (1: no workspace)

@@ -256,7 +256,7 @@ lb_status lb_lora_workspace(int64_t rows, int32_t d_in, int32_t d_out, int32_t r
     need(rows >= 0 && rows <= (1 << 28), "rows must be in 0..2^28");
     need(rank >= 8 && rank <= 128 && rank % 8 == 0, "rank must be a multiple of 8, at most 128");
     need(d_in >= 8 && d_in % 8 == 0 && d_out >= 8 && d_out % 8 == 0, "d_in and d_out must be positive multiples of 8");
-    *bytes = rows * rank * 4;
+    *bytes = lora_whole(rows, d_in, d_out, rank) ? 0 : rows * rank * 4;
     return hipSuccess;
   });
 }
@@ -281,7 +281,7 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     if (rows == 0) return hipSuccess;
     need(((rows + 15) / 16) * ((d_out + 255) / 256) <= kMostGroups, "too much work for one call: rows * d_out is too large");
     LoraArgs A{};
-    need(workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4,
+    need(lora_whole(rows, d_in, d_out, rank) || (workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says");
     A.x = x;
     A.y = y;

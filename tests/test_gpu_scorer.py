@@ -411,6 +411,13 @@ LORA = [  # rows, d_in, d_out, rank, adapters, ids, type
     (50, 136, 64, 96, 60, "each", "bf16"),
     (300, 72, 40, 32, 3, "none", "f32"),
     (5, 4096, 8, 8, 2, "each", "f16"),
+    # one launch or two, the rank's tiles side by side or not, a rank that ends inside a tile
+    (256, 200, 1024, 16, 9, "each", "f32"),
+    (257, 200, 1024, 16, 9, "each", "bf16"),
+    (70, 2048, 1032, 32, 5, "runs", "bf16"),
+    (21, 2040, 600, 32, 5, "each", "f32"),
+    (9, 64, 2000, 120, 3, "each", "f16"),
+    (1030, 96, 272, 56, 4, "runs", "f16"),
 ]
 
 

@@ -123,7 +123,7 @@ def test_empty_batches_are_nothing_to_do():
                                       (6, AT + 4), (7, 63), (7, 65), (8, None), (9, 8), (10, None), (11, AT + 8), (12, None),
                                       (14, None), (15, 60), (16, None), (16, AT + 8), (17, 100)])
 def test_lora_that_is_refused(at, value):
-    a = [0, 4, 64, 64, 16, 2, AT, 64, AT, 64, AT, AT, AT, None, 2 * AT, 64, AT, 1 << 20, None]
+    a = [0, 300, 64, 64, 16, 2, AT, 64, AT, 64, AT, AT, AT, None, 2 * AT, 64, AT, 1 << 20, None]
     a[at] = value
     assert refused(lbm.lib().lb_lora_add(*a))
 
@@ -134,6 +134,8 @@ def test_lora_in_place_needs_the_same_stride():
     for bad in ((-1, 64, 64, 16), (4, 63, 64, 16), (4, 64, 0, 16), (4, 64, 64, 200)):
         assert refused(lbm.lib().lb_lora_workspace(*bad, ctypes.addressof(n)))
     assert refused(lbm.lib().lb_lora_workspace(4, 64, 64, 16, None))
+    for rows, d_out, rank, some in ((4, 64, 16, False), (300, 64, 16, True), (4, 2048, 16, True), (4, 64, 64, True)):
+        assert lbm.lib().lb_lora_workspace(rows, 64, d_out, rank, ctypes.addressof(n)) == lbm.LB_OK and (n.value > 0) == some
 
 
 def rules(**over):
