@@ -220,10 +220,10 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
     if (both && ch >= half) return;
     float x[4][8], y[4][8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) load8(src + row[t] * A.q_stride, x[t]);
+    for (int t = 0; t < 4; ++t) load8_nt(src + row[t] * A.q_stride, x[t]);
     if (both) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) load8(src + row[t] * A.q_stride + half, y[t]);
+      for (int t = 0; t < 4; ++t) load8_nt(src + row[t] * A.q_stride + half, y[t]);
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         float cs[8], sn[8];
@@ -253,8 +253,8 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       if (live[t]) {
-        store8(dst + row[t] * A.q_out_stride, x[t]);
-        if (both) store8(dst + row[t] * A.q_out_stride + half, y[t]);
+        store8_nt(dst + row[t] * A.q_out_stride, x[t]);
+        if (both) store8_nt(dst + row[t] * A.q_out_stride + half, y[t]);
       }
     return;
   }
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
     const T* src = static_cast<const T*>(A.k) + h * D + ch;
     float x[4][8];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) load8(src + row[t] * A.k_stride, x[t]);
+    for (int t = 0; t < 4; ++t) load8_nt(src + row[t] * A.k_stride, x[t]);
     if ((ch & ~31) >= A.rot) {  // the whole block stays: the four lanes of a block go the same way
 #pragma unroll
       for (int t = 0; t < 4; ++t) value_block(x[t], codes[t], scale[t]);
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
         } else {
           float y[8], cs[8], sn[8];
           const bool low = ch < half;
-          load8(src + row[t] * A.k_stride + (low ? half : -half), y);
+          load8_nt(src + row[t] * A.k_stride + (low ? half : -half), y);
           load8(A.cos + angles + (low ? ch : ch - half), cs);
           load8(A.sin + angles + (low ? ch : ch - half), sn);
 #pragma unroll
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
   const T* src = static_cast<const T*>(A.v) + h * D + ch;
   float x[4][8];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) load8(src + row[t] * A.v_stride, x[t]);
+  for (int t = 0; t < 4; ++t) load8_nt(src + row[t] * A.v_stride, x[t]);
 #pragma unroll
   for (int t = 0; t < 4; ++t) value_block(x[t], codes[t], scale[t]);
   if (!live_item) return;
@@ -533,18 +533,24 @@ struct Pages {
   __device__ __forceinline__ int32_t slot(int32_t t, int u) const { return (begin + t * 32 + 16 * u) & ((1 << shift) - 1); }
 };
 
-// N words from memory that is aligned to as many (2 or 4: in one load)
-template <int N>
+template <bool once, typename V>
+__device__ __forceinline__ V load_as(const uint8_t* p) {
+  const V* at = reinterpret_cast<const V*>(p);
+  if constexpr (once) return __builtin_nontemporal_load(at);
+  return *at;
+}
+// N words from memory that is aligned to as many (2 or 4: in one load); once: they are read by nobody else
+template <int N, bool once = false>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
   if constexpr (N == 1) {
-    w[0] = *reinterpret_cast<const uint32_t*>(p);
+    w[0] = load_as<once, uint32_t>(p);
   } else if constexpr (N == 2) {
-    const u32x2 a = *reinterpret_cast<const u32x2*>(p);
+    const u32x2 a = load_as<once, u32x2>(p);
     w[0] = a.x, w[1] = a.y;
   } else {
 #pragma unroll
     for (int c = 0; c < N; c += 4) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(p + 4 * c);
+      const u32x4 a = load_as<once, u32x4>(p + 4 * c);
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[c + x] = a[x];
     }
@@ -580,6 +586,7 @@ struct Keys {
   }
 
   // loads tile t; bit u of the result: half u exists
+  template <bool once>
   __device__ __forceinline__ int load(int32_t t, Tile<D>& X, uint32_t* flags) {
     int32_t page[2];
     P.of(t, page, flags);
@@ -591,8 +598,8 @@ struct Keys {
       const int32_t slot = P.slot(t, u);
       const uint8_t* at = base + page[u] * page_bytes + slot * (D / 2);
       const uint8_t* scales = base + page[u] * page_bytes + slot * (D / 32);
-      load_words<D / 32>(at + k_at, X.k[u]);
-      load_words<D / 32>(at + v_at, X.v[u]);
+      load_words<D / 32, once>(at + k_at, X.k[u]);
+      load_words<D / 32, once>(at + v_at, X.v[u]);
       X.ks[u] = D == 256 ? *reinterpret_cast<const uint16_t*>(scales + ks_at) : scales[ks_at];
       X.vs[u] = *reinterpret_cast<const uint32_t*>(scales + vs_at);
     }
@@ -804,11 +811,12 @@ struct Rows {
   }
 
   // All tiles of a key range, the next tile's loads in flight during each.
+  template <bool once>
   __device__ __forceinline__ void sweep(Keys<D>& K, int32_t t, int32_t t_hi, int j, uint32_t* flags) {
     Tile<D> X{}, Y{};
-    int ok = t < t_hi ? K.load(t, X, flags) : 0;
+    int ok = t < t_hi ? K.template load<once>(t, X, flags) : 0;
     for (; t < t_hi; t += K.P.step) {
-      const int next = t + K.P.step < t_hi ? K.load(t + K.P.step, Y, flags) : 0;
+      const int next = t + K.P.step < t_hi ? K.template load<once>(t + K.P.step, Y, flags) : 0;
       const int32_t tb = K.P.begin + t * 32;
       take(X, tb, ok, j);
       X = Y;
@@ -941,13 +949,15 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend_short
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
   Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
-  S.sweep(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
+  S.template sweep<false>(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
   store_rows<D, T, 1>(A, w, w.tile * 16, S, n, j);
 }
 
 // Few query rows: a workgroup takes 16 rows and one part of their key range; its
-// four wavefronts take every fourth tile and join at the end.
-template <int D, typename T>
+// four wavefronts take every fourth tile and join at the end.  once: nobody else
+// reads the keys, which then leave the caches to others (4 x 110 000 keys of 8 heads:
+// 88 us, else 98).
+template <int D, typename T, bool once>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
@@ -961,7 +971,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
   const int32_t tiles = S.end > begin ? (S.end - begin + 31) >> 5 : 0;
   const int32_t per = (tiles + A.splits - 1) / A.splits;
   Keys<D> K(A.kv, w.s, w.h, begin, S.end, 4, n, j);
-  S.sweep(K, split * per + wave, min(tiles, (split + 1) * per), j, A.kv.flags);
+  S.template sweep<once>(K, split * per + wave, min(tiles, (split + 1) * per), j, A.kv.flags);
   const float l = row_sum(S.l[0]);
 
   // join the four wavefronts
@@ -1289,7 +1299,11 @@ hipError_t attend(const AttendArgs& A, hipStream_t st) {
     k_attend_short<D, T><<<dim3(static_cast<unsigned>((jobs + 3) / 4)), 256, 0, st>>>(A);
     return hipGetLastError();
   }
-  k_attend<D, T><<<dim3(static_cast<unsigned>(jobs * A.splits)), 256, 0, st>>>(A);
+  const dim3 grid(static_cast<unsigned>(jobs * A.splits));
+  if (A.tiles == 1 && A.splits > 1)
+    k_attend<D, T, true><<<grid, 256, 0, st>>>(A);
+  else
+    k_attend<D, T, false><<<grid, 256, 0, st>>>(A);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.splits == 1) return e;
   k_attend_join<D, T><<<dim3(static_cast<unsigned>(jobs * A.part_rows)), 256, 0, st>>>(A);
@@ -1316,7 +1330,8 @@ hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStr
 // exist (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8
 // heads take 99 us with them, 101 with six, 106 with eight), each with 16 tiles of
 // keys at least; where there are many such jobs with at most 16 tiles of keys, a
-// wavefront takes one alone (ALONE_FIGURES).  The others: a workgroup takes the
+// wavefront takes one alone (1024 sequences of 3 to 256 keys, 4 heads of 64: 16 us,
+// else 26).  The others: a workgroup takes the
 // rows of its four wavefronts, and the workgroups are numbered as append's units
 // are, so that a ragged batch has no more than one idle one a sequence and head.  A
 // batch that may hold both gets both kernels, each of which leaves the other's

@@ -241,6 +241,8 @@ struct Part {
     }
   }
 
+  // once: the row is not read again
+  template <bool once>
   __device__ __forceinline__ Sum sum(int32_t target, float* xt) const {
     Sum s{-__builtin_inff(), 0.0f};
     // whole chunks, two at a time: two loads on their way, and one rescaling for both
@@ -249,8 +251,13 @@ struct Part {
     if (c == 0 && first < lo && c < chunks) one(s, c), c += 256;
     for (; c + 256 < last; c += 512) {
       float x[16];
-      load8(src + first + 8 * c, *reinterpret_cast<float(*)[8]>(x));
-      load8(src + first + 8 * (c + 256), *reinterpret_cast<float(*)[8]>(x + 8));
+      if constexpr (once) {
+        load8_nt(src + first + 8 * c, *reinterpret_cast<float(*)[8]>(x));
+        load8_nt(src + first + 8 * (c + 256), *reinterpret_cast<float(*)[8]>(x + 8));
+      } else {
+        load8(src + first + 8 * c, *reinterpret_cast<float(*)[8]>(x));
+        load8(src + first + 8 * (c + 256), *reinterpret_cast<float(*)[8]>(x + 8));
+      }
       if (sparse) {
         mask(*reinterpret_cast<float(*)[8]>(x), open[c]);
         mask(*reinterpret_cast<float(*)[8]>(x + 8), open[c + 256]);
@@ -302,7 +309,7 @@ struct Part {
 
 // One part of a row: its sum, and all the rest where the row has one part.  The
 // parts' sums are kept at part[row][split] = (m, l), the target's logit after them.
-template <typename T>
+template <typename T, bool once>
 __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
   extern __shared__ uint32_t shared[];
   __shared__ float xt;
@@ -313,7 +320,7 @@ __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
   P.start(A, row, part, A.splits, slots, shared);
   const int32_t target = A.score ? A.target[row] : -1;
   if (!P.sparse) __syncthreads();  // xt
-  Sum s = block_sum(P.sum(target, &xt), P.k);  // its barrier also shows xt to all
+  Sum s = block_sum(P.template sum<once>(target, &xt), P.k);  // its barrier also shows xt to all
   if (A.splits > 1) {
     if (threadIdx.x == 0) {
       A.part[2 * (row * A.splits + part)] = s.m;
@@ -497,7 +504,11 @@ hipError_t run(const LogitArgs& A, hipStream_t st) {
   const int64_t most = (int64_t{1} << 23) / A.splits;
   for (LogitArgs B = A; B.row0 < A.rows; B.row0 += most) {
     const int64_t rows = A.rows - B.row0 < most ? A.rows - B.row0 : most;
-    k_logits<T><<<dim3(static_cast<unsigned>(rows * A.splits)), 256, lds, st>>>(B, slots);
+    const dim3 grid(static_cast<unsigned>(rows * A.splits));
+    if (A.logprobs)
+      k_logits<T, false><<<grid, 256, lds, st>>>(B, slots);
+    else
+      k_logits<T, true><<<grid, 256, lds, st>>>(B, slots);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (A.splits == 1) continue;

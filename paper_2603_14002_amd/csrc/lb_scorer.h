@@ -148,6 +148,44 @@ __device__ __forceinline__ void store8(_Float16* p, const float (&x)[8]) {
   *reinterpret_cast<f16x8*>(p) = w;
 }
 
+// The same for what is read once and what is not read again soon: it does not
+// push other data out of the caches.
+__device__ __forceinline__ void load8_nt(const float* p, float (&x)[8]) {
+  const f32x4 a = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + 4));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+__device__ __forceinline__ void load8_nt(const __bf16* p, float (&x)[8]) {
+  const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8_nt(const _Float16* p, float (&x)[8]) {
+  const f16x8 w = __builtin_nontemporal_load(reinterpret_cast<const f16x8*>(p));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(w[i]);
+}
+
+__device__ __forceinline__ void store8_nt(float* p, const float (&x)[8]) {
+  __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, reinterpret_cast<f32x4*>(p + 4));
+}
+__device__ __forceinline__ void store8_nt(__bf16* p, const float (&x)[8]) {
+  bf16x8 w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = static_cast<__bf16>(x[i]);
+  __builtin_nontemporal_store(w, reinterpret_cast<bf16x8*>(p));
+}
+__device__ __forceinline__ void store8_nt(_Float16* p, const float (&x)[8]) {
+  f16x8 w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = static_cast<_Float16>(x[i]);
+  __builtin_nontemporal_store(w, reinterpret_cast<f16x8*>(p));
+}
+
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }

@@ -123,11 +123,11 @@ def _empty(shape, dtype, like, stream):
     comes from that stream's own pool (a block of the current stream's pool may still be in use by work queued
     there), and it is also kept for work that the current stream has been given when it is dropped."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return torch.empty(*shape, dtype=dtype, device=like.device)  # sizes one by one: parsed sooner than a tuple
     with torch.cuda.device(like.device):
         here = torch.cuda.current_stream()
         with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
-            t = torch.empty(shape, dtype=dtype, device=like.device)
+            t = torch.empty(*shape, dtype=dtype, device=like.device)
         t.record_stream(here)
     return t
 
@@ -141,7 +141,7 @@ def _scratch(like, stream, nbytes: int, given, name: str):
         return given.data_ptr(), given.numel() * given.element_size(), given
     if nbytes == 0:
         return None, 0, None
-    ws = _empty(nbytes, torch.uint8, like, stream)
+    ws = _empty((nbytes,), torch.uint8, like, stream)
     return ws.data_ptr(), nbytes, ws
 
 
@@ -449,8 +449,8 @@ def lb_logits_adjust(logits, rules: Optional[LogitRules] = None, target=None, wa
         _ints(target, "target", (rows,))
         if target.get_device() != g:
             _elsewhere(g, target=target)
-        score = _empty(rows, torch.float32, logits, stream)
-    lse = _empty(rows, torch.float32, logits, stream)
+        score = _empty((rows,), torch.float32, logits, stream)
+    lse = _empty((rows,), torch.float32, logits, stream)
     ref = None
     if rules is not None:
         h, b, m, r = rules.history, rules.bias_ids, rules.mask, rules.mask_row
