@@ -222,7 +222,8 @@ enum { LB_MAX_RULE_IDS = 4096 };
  * (each may be NULL; target is read if score is not).  Masked classes get
  * -infinity whatever their logits hold, a row with nothing left -infinity
  * throughout.  rules NULL: none.
- *   logits    device [rows][classes] of `dtype`, row stride logits_stride
+ *   logits    device [rows][classes] of `dtype`, row stride logits_stride; rows at
+ *             most 2^28, classes 2^30
  *   workspace  device, 16-B aligned, at least what lb_logits_workspace says for
  *              these rows and classes (NULL if that is 0)
  * logits is only read; logprobs may be the logits themselves where these are

@@ -829,7 +829,6 @@ struct Rows {
 // spilling (o and q take 4 D/16 + 4 D/32 NP registers a row tile).
 constexpr int waves(int D, int pieces, int QT) { return D * QT * (1 + pieces) <= 256 ? 3 : D * QT * (1 + pieces) <= 768 ? 2 : 1; }
 
-constexpr int kFewRows = 64;      // query rows of a sequence and KV head that the few-row kernel takes
 constexpr int kMostSplits = 128;  // parts of a key range
 
 // query row tiles of 16 a wavefront holds where there are many rows
@@ -852,7 +851,7 @@ __device__ __forceinline__ Job few_job(const AttendArgs& A, uint32_t job) {
   w.q = sequence(A.kv, w.s);
   w.G = A.kv.q_heads / A.kv.kv_heads;
   w.R = w.q.count * w.G;
-  if (w.R > kFewRows) w.R = 0;  // the many-row kernel's
+  if (w.R > A.few_rows) w.R = 0;  // the many-row kernel's
   return w;
 }
 // every sequence has a job of tile 0 and head 0
@@ -1132,14 +1131,14 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows
   constexpr int KA = ahead(D, NP, QT, 2 * KC), VA = ahead(D, NP, QT, VC);
   __shared__ Shared<D> L;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
-  if (!A.few) check_sequence(A.kv, blockIdx.x);
+  if (A.few_rows == 0) check_sequence(A.kv, blockIdx.x);
   Job w;
   w.G = A.kv.q_heads / A.kv.kv_heads;
   w.h = static_cast<int32_t>(blockIdx.x % A.kv.kv_heads);
   w.s = row_unit(A.kv, static_cast<int32_t>(blockIdx.x / A.kv.kv_heads), w.G, per, &w.tile);
   w.q = sequence(A.kv, w.s);
   w.R = w.q.count * w.G;
-  if (A.few && w.R <= kFewRows) return;  // the few-row kernel's
+  if (w.R <= A.few_rows) return;  // the few-row kernel's
   const int32_t tiles_of_rows = (w.R + per - 1) / per;
   if (w.tile < 0 || w.tile >= tiles_of_rows) return;
   w.tile = tiles_of_rows - 1 - w.tile;  // the last rows see most keys: they go first
@@ -1292,7 +1291,7 @@ hipError_t attend(const AttendArgs& A, hipStream_t st) {
     const int64_t blocks = A.units * A.kv.kv_heads;
     k_attend_rows<D, T, row_tiles(D, Pieces<T>::n)><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !A.few) return e;
+    if (e != hipSuccess || A.few_rows == 0) return e;
   }
   const int64_t jobs = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads;
   if (A.alone) {
@@ -1325,28 +1324,35 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(read); }
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st) { LB_KV_DISPATCH(attend); }
 
-// How a call is cut up.  Sequences with at most kFewRows query rows a KV head:
-// tiles of 16 rows, and parts of the key range so that about three workgroups a CU
-// exist (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8
-// heads take 99 us with them, 101 with six, 106 with eight), each with 16 tiles of
-// keys at least; where there are many such jobs with at most 16 tiles of keys, a
-// wavefront takes one alone (1024 sequences of 3 to 256 keys, 4 heads of 64: 16 us,
-// else 26).  The others: a workgroup takes the
-// rows of its four wavefronts, and the workgroups are numbered as append's units
-// are, so that a ragged batch has no more than one idle one a sequence and head.  A
-// batch that may hold both gets both kernels, each of which leaves the other's
-// sequences alone.
+constexpr int64_t kLeastGroups = 600;  // of 128 rows
+
+// How a call is cut up.  Sequences with at most few_rows query rows a KV head: tiles
+// of 16 rows, and parts of the key range so that about three workgroups a CU exist
+// (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8 heads
+// take 99 us with them, 101 with six, 106 with eight), each with 16 tiles of keys at
+// least; where there are many such jobs with at most 16 tiles of keys, a wavefront
+// takes one alone (1024 sequences of 3 to 256 keys, 4 heads of 64: 16 us, else 26).
+// The others: a workgroup takes the rows of its four wavefronts, and the workgroups
+// are numbered as append's units are, so that a ragged batch has no more than one
+// idle one a sequence and head.  A batch that may hold both gets both kernels, each
+// of which leaves the other's sequences alone.  The many-row kernel does an
+// eighth of the conversions, but it has no parts of keys: with fewer rows than fill
+// the chip (512 workgroups of 128 rows are resident) all goes to the other (8 KV heads
+// of 128 channels, 4 query heads each, bf16: 100 new tokens of 20 000, 25 groups of
+// 128 rows, 99 us, else 772; 1000 of 5000, 250 groups, 151 us, else 201; 3000 of 3000,
+// 750 groups, 170 us, else 127).
 AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   AttendPlan p{};
   const int64_t G = kv.q_heads / kv.kv_heads, rows = kv.max_new * G;
+  const int64_t units = kv.n_rows * G / (4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3)) + kv.n_seqs;
   p.splits = 1;
-  if (rows > kFewRows) {
-    const int64_t per = 4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3);
-    p.units = kv.n_rows * G / per + kv.n_seqs;
-    if (kv.n_seqs == 1) return p;
+  p.few_rows = 0x7FFFFFFF;
+  if (rows > 64 && kv.n_rows * G * kv.kv_heads >= 128 * kLeastGroups) {
+    p.units = units;
+    p.few_rows = kv.n_seqs == 1 ? 0 : 64;
+    if (p.few_rows == 0) return p;
   }
-  p.few = true;
-  const int64_t most = rows < kFewRows ? rows : kFewRows;
+  const int64_t most = rows < p.few_rows ? rows : p.few_rows;
   p.tiles = static_cast<int32_t>((most + 15) / 16);
   p.part_rows = static_cast<int32_t>(most < 16 ? most : 16);
   const int64_t jobs = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;

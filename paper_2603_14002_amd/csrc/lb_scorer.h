@@ -49,7 +49,8 @@ struct AttendArgs {
   // the plan's
   int32_t tiles, splits, part_rows;
   int64_t units, part_sums;
-  bool few, alone;
+  int32_t few_rows;
+  bool alone;
 };
 
 struct LoraArgs {
@@ -74,12 +75,14 @@ struct LogitArgs {
   lb_logit_rules r;
 };
 
-// How an attention call is cut up (see attend_plan).  Few-row kernel: `few`, tiles
-// of 16 query rows a sequence and KV head, whether a wavefront takes one alone, the parts that a key range is cut into,
-// the rows of a tile whose parts are kept, the floats of these and where the parts'
-// sums start among them.  Many-row kernel: its units of rows, 0: none.
+// How an attention call is cut up (see attend_plan).  Few-row kernel: the query rows
+// of a sequence and KV head up to which it takes them (0: it does not run), tiles of
+// 16 rows, whether a wavefront takes one alone, the parts that a key range is cut
+// into, the rows of a tile whose parts are kept, the floats of these and where the
+// parts' sums start among them.  Many-row kernel: its units of rows, 0: none.
 struct AttendPlan {
-  bool few, alone;
+  int32_t few_rows;
+  bool alone;
   int32_t tiles, splits, part_rows;
   int64_t part_floats, part_sums, units;
 };

@@ -244,7 +244,7 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     A.part_rows = p.part_rows;
     A.units = p.units;
     A.part_sums = p.part_sums;
-    A.few = p.few;
+    A.few_rows = p.few_rows;
     A.alone = p.alone;
     return launch_kv_attend(A, cache->head_dim, dtype, static_cast<hipStream_t>(stream));
   });
@@ -306,7 +306,7 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
 lb_status lb_logits_workspace(int64_t rows, int32_t classes, int64_t* bytes) {
   return entry([&] {
     need(bytes != nullptr, "null host pointer");
-    need(rows >= 0 && rows <= (1 << 28) && classes >= 1, "rows must be in 0..2^28, classes at least 1");
+    need(rows >= 0 && rows <= (1 << 28) && classes >= 1 && classes <= (1 << 30), "rows must be in 0..2^28, classes in 1..2^30");
     const int64_t s = logits_splits(rows, classes);
     *bytes = s > 1 ? (rows * s * 2 + rows) * 4 : 0;
     return hipSuccess;
@@ -319,7 +319,7 @@ lb_status lb_logits_adjust(int32_t dtype, int64_t rows, int32_t classes, const v
                            int64_t workspace_bytes, void* stream) {
   return entry([&] {
     check_dtype(dtype);
-    need(rows >= 0 && rows <= (1 << 28) && classes >= 1, "rows must be in 0..2^28, classes at least 1");
+    need(rows >= 0 && rows <= (1 << 28) && classes >= 1 && classes <= (1 << 30), "rows must be in 0..2^28, classes in 1..2^30");
     need(logits || rows == 0, "null device pointer: logits");
     need(logits_stride >= classes && logits_stride <= (int64_t{1} << 40), "logits_stride must be at least classes");
     need(reinterpret_cast<uintptr_t>(logits) % size_of(dtype) == 0, "logits must be aligned to their type");

@@ -117,14 +117,15 @@ def attend(q, k, v, scale, first, window):
         lo = max(0, p - window + 1) if window else 0
         if p < 0 or lo > min(p, n - 1):
             continue
-        for h in range(Hq):
-            kk, vv = k[lo:p + 1, h // (Hq // H)], v[lo:p + 1, h // (Hq // H)]
-            s = (kk @ q[i, h]) * scale
-            lse[i, h] = torch.logsumexp(s, 0)
-            w = torch.exp(s - lse[i, h])
-            out[i, h] = w @ vv
-            mass[i, h] = w @ vv.abs()
-            reach[i, h] = ((kk.abs() @ q[i, h].abs()) * abs(scale)).max()
+        for g in range(H):
+            heads = slice(g * (Hq // H), (g + 1) * (Hq // H))
+            kk, vv = k[lo:p + 1, g], v[lo:p + 1, g]
+            s = (q[i, heads] @ kk.t()) * scale
+            lse[i, heads] = torch.logsumexp(s, 1)
+            w = torch.exp(s - lse[i, heads, None])
+            out[i, heads] = w @ vv
+            mass[i, heads] = w @ vv.abs()
+            reach[i, heads] = ((q[i, heads].abs() @ kk.abs().t()) * abs(scale)).amax(1)
     return out, lse, mass, reach
 
 

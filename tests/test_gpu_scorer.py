@@ -241,6 +241,14 @@ ATTEND = [  # new, length, page, q heads, kv heads, D, window, type, padding row
     ([150, 1], [333, 700], 16, 3, 1, 128, 64, "f32", 0),
     ([70, 3], [90, 5], 16, 2, 1, 256, 2 ** 31 - 1, "f32", 0),
     ([66, 1], [70, 1], 128, 5, 1, 256, 0, "f16", 0),
+    # enough rows for the kernel that takes many, with sequences of few rows beside and without
+    ([700], [800], 32, 112, 16, 64, 0, "bf16", 1),
+    ([650, 1, 3, 0, 40], [650, 1500, 64, 7, 300], 16, 128, 8, 64, 0, "bf16", 2),
+    ([310, 300], [330, 333], 64, 128, 4, 128, 90, "bf16", 0),
+    ([301, 1], [320, 900], 16, 256, 8, 64, 0, "f16", 0),
+    ([300, 2], [300, 400], 32, 260, 4, 128, 17, "f32", 0),
+    ([305], [306], 128, 256, 2, 256, 0, "bf16", 0),
+    ([160, 140, 2], [160, 200, 200], 16, 256, 4, 256, 0, "f32", 3),
 ]
 # What the probabilities' pieces leave: bf16 has 8 significant bits, so a piece is off by at most half a step, 2^-8 of
 # what it stands for, and 1, 2 and 3 pieces by 2^-8, 2^-16 and 2^-24.
@@ -297,11 +305,13 @@ def test_attend(case):
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
-@pytest.mark.parametrize("new,D", [(1, 64), (12, 128), (40, 64), (48, 128), (45, 256)])
-def test_attend_unseen_tokens_have_no_effect(t, new, D):
+@pytest.mark.parametrize("new,D,Hq", [(1, 64, 4), (12, 128, 4), (40, 64, 4), (48, 128, 4), (45, 256, 4),
+                                      (310, 64, 256), (310, 128, 256), (310, 256, 256)])
+def test_attend_unseen_tokens_have_no_effect(t, new, D, Hq):
     """NaN keys and values past a row's position reach no row before them; those a row sees make it NaN."""
     rng = np.random.default_rng(8)
-    n = 50
+    n = max(50, new + 7)
+    G = Hq // 2
     R = ref.Ragged([new, 1], [n, 20], 16, 2, D, seed=9)
     k, v = randn(rng, n, 2, D, dtype=torch.float64), randn(rng, n, 2, D, dtype=torch.float64)
     if new > 1:
@@ -311,7 +321,7 @@ def test_attend_unseen_tokens_have_no_effect(t, new, D):
         v[3, 1, 40] = math.nan
     R.put(0, k, v)
     R.put(1, randn(rng, 20, 2, D, dtype=torch.float64), randn(rng, 20, 2, D, dtype=torch.float64))
-    q = dev(randn(rng, new + 1, 4, D, dtype=DT[t]))
+    q = dev(randn(rng, new + 1, Hq, D, dtype=DT[t]))
     cache, batch = handles(R)
     say(f"[case] unseen {t} {new} {D}")
     out, lse = lbm.lb_kv_attend(cache, batch, q, 0.2, want_lse=True)
@@ -319,10 +329,10 @@ def test_attend_unseen_tokens_have_no_effect(t, new, D):
     o = out.cpu()
     if new > 1:
         assert bool(torch.isfinite(o[:new - 5]).all())
-        assert bool(torch.isnan(o[new - 5:new, :2]).all()) and bool(torch.isnan(o[new - 4:new, 2:, 32:64]).all())
-        assert bool(torch.isfinite(o[:new, 2:, :32]).all()) and bool(torch.isfinite(lse[:new, 2:]).all())
+        assert bool(torch.isnan(o[new - 5:new, :G]).all()) and bool(torch.isnan(o[new - 4:new, G:, 32:64]).all())
+        assert bool(torch.isfinite(o[:new, G:, :32]).all()) and bool(torch.isfinite(lse[:new, G:]).all())
     else:
-        assert bool(torch.isnan(o[0, 2:, 32:64]).all()) and bool(torch.isfinite(o[0, :, :32]).all())
+        assert bool(torch.isnan(o[0, G:, 32:64]).all()) and bool(torch.isfinite(o[0, :, :32]).all())
     assert bool(torch.isfinite(o[new:]).all())
 
 
