@@ -13,7 +13,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblightbeam.so")
-SOURCES = ["lb_kernels.hip", "lb_api.cpp", "lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer_api.cpp"]
+SOURCES = ["lb_kernels.hip", "lb_host.cpp", "lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer_api.cpp"]
 # k_decode loops over frames: machine-level hoisting of loop-invariant values
 # out of that loop keeps them live across it and makes the kernel spill
 EXTRA = {"lb_kernels.hip": ["-mllvm", "-disable-machine-licm"]}
@@ -31,7 +31,7 @@ COMMON = [
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 DECODER = [os.path.join(CSRC, f) for f in ("lb_kernels.hip", "lb_device.h", "lb_launch.h", "lb_api.cpp")] + \
     [os.path.join(INCLUDE, "lightbeam.h")]
-HASHED = DECODER + [os.path.join(CSRC, f) for f in ("lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer.h",
+HASHED = DECODER + [os.path.join(CSRC, f) for f in ("lb_host.cpp", "lb_kv.hip", "lb_logits.hip", "lb_lora.hip", "lb_scorer.h",
                                                     "lb_scorer_api.cpp")] + \
     [os.path.join(INCLUDE, "lightbeam_scorer.h")]
 

@@ -30,15 +30,6 @@ lb_status fail(lb_status st, const std::string& msg) {
   return st;
 }
 
-}  // namespace
-
-// lb_last_error's message, set by the library's other files
-namespace lb {
-lb_status set_last_error(lb_status st, const std::string& msg) { return fail(st, msg); }
-}  // namespace lb
-
-namespace {
-
 #define LB_HIP(call)                                                                  \
   do {                                                                                \
     hipError_t e_ = (call);                                                           \

@@ -12,7 +12,7 @@
 #include "lb_scorer.h"
 
 namespace lb {
-lb_status set_last_error(lb_status st, const std::string& msg);  // lb_api.cpp
+lb_status set_last_error(lb_status st, const std::string& msg);  // lb_host.cpp
 }
 
 using namespace lb;
