@@ -171,7 +171,10 @@ __device__ __forceinline__ uint32_t bytes_at(const uint32_t (&w)[4], int i) {
 // A workgroup takes a unit (four positions of a sequence) and 256 of its (head,
 // eight channels) items: queries, then keys, then values.  A lane has its
 // channels of all four tokens in flight, and the four lanes of a block of 32
-// channels agree on the scale by two quad moves.
+// channels agree on the scale by two quad moves.  24 000 tokens of 12 prompts, 32 + 16
+// heads of 128, bf16: 116 us, 4.5 TB/s; what the rows wait for (starts, lengths, page)
+// and the registers of the 64-bit rotation bound it.  Rows are read and written once,
+// past the caches (else 128 us).
 template <int D, typename T>
 __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
   int32_t group;
@@ -351,6 +354,8 @@ __device__ __forceinline__ void values8(uint32_t codes, uint32_t byte, float (&x
   x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
 }
 
+// The same units and items, the other way.  24 000 tokens, 16 heads of 128, bf16: 22
+// us, 5.7 TB/s, bound by memory.
 template <int D, typename T>
 __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
   int32_t group;
@@ -1029,6 +1034,10 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
 // from memory.  A ring of 2 A tiles has a barrier every A tiles: at step t the keys
 // of t + 1 and the values of t are read, made A steps or more before, and those of t
 // + 1 + A and t + A are made, in places that were last read A steps or more before.
+// Six prompts of 65..2048 tokens over 130..4096, 32 heads of 128 on 8, bf16: 343 us,
+// 680 TFLOP/s; vector instructions are issued in half of the SIMD cycles (a lane's
+// eight scores of a row take 8 products, exponentials and sums each), matrix ones run
+// in 29 %, and two wavefronts a SIMD do not cover each other's waits.
 template <int D>
 struct Shared {
   static constexpr int KC = D / 32, VC = D / 16;
