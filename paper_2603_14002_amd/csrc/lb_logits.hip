@@ -115,23 +115,24 @@ __device__ __forceinline__ Sum block_sum(Sum s, float k) {
   for (int w = 1; w < 4; ++w) join(t, sm[w], sl[w], k);
   return t;
 }
-// The log-sum-exp as its reference (a logit) and the rest (a power of two): log p =
-// ln2 (k (x - m) - rest) stays right where m is so large that m + rest is m.
+// The log-sum-exp as its reference m (a logit before the temperature) and the rest:
+// log p = (x - m) / temperature - rest stays right where m is so large that m + rest
+// is m.  The quotient is a product with the rounded reciprocal.
 struct Lse {
-  float m, rest;
-  __device__ __forceinline__ float value(float temperature) const { return m / temperature + rest * kLn2; }
+  float m, rest, inv;
+  __device__ __forceinline__ float value() const { return fmaf(m, inv, rest); }
 };
-__device__ __forceinline__ Lse log_sum(Sum s) { return {safe(s.m), s.l == 0.0f ? -__builtin_inff() : log2f(s.l)}; }
-__device__ __forceinline__ float log_prob(float x, float k, Lse lse) {
-  return x == -__builtin_inff() ? x : ((x - lse.m) * k - lse.rest) * kLn2;
+__device__ __forceinline__ Lse log_sum(Sum s, float temperature) {
+  return {safe(s.m), s.l == 0.0f ? -__builtin_inff() : log2f(s.l) * kLn2, 1.0f / temperature};
 }
+__device__ __forceinline__ float log_prob(float x, Lse lse) { return x == -__builtin_inff() ? x : fmaf(x - lse.m, lse.inv, -lse.rest); }
 
 // xt: the target's logit after the rules up to the temperature
-__device__ __forceinline__ void finish(const LogitArgs& A, int64_t row, Lse lse, float xt, float k) {
-  if (A.lse) A.lse[row] = lse.value(A.r.temperature);
+__device__ __forceinline__ void finish(const LogitArgs& A, int64_t row, Lse lse, float xt) {
+  if (A.lse) A.lse[row] = lse.value();
   if (!A.score) return;
   const int32_t t = A.target[row];
-  A.score[row] = t < 0 ? 0.0f : t >= A.classes ? __builtin_nanf("") : log_prob(xt, k, lse);
+  A.score[row] = t < 0 ? 0.0f : t >= A.classes ? __builtin_nanf("") : log_prob(xt, lse);
 }
 
 // ------------------------------------------------------------------ long rows
@@ -292,7 +293,7 @@ struct Part {
       float x[8];
       const bool whole = load(c, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = log_prob(x[i], k, lse);
+      for (int i = 0; i < 8; ++i) x[i] = log_prob(x[i], lse);
       const int32_t w = first + 8 * c;
       if (whole && even) {
         store8(dst + w, x);
@@ -305,7 +306,7 @@ struct Part {
     if (!slots) return;
     __syncthreads();  // the named classes' places have been written above, as masked
     for (int32_t i = threadIdx.x; i < slots; i += 256)
-      if (table[i].id >= 0) dst[table[i].id] = log_prob(table[i].x, k, lse);
+      if (table[i].id >= 0) dst[table[i].id] = log_prob(table[i].x, lse);
   }
 };
 
@@ -331,8 +332,8 @@ __global__ __launch_bounds__(256) void k_logits(LogitArgs A, int32_t slots) {
     }
     return;
   }
-  const Lse lse = log_sum(s);
-  if (threadIdx.x == 0) finish(A, row, lse, xt, P.k);
+  const Lse lse = log_sum(s, A.r.temperature);
+  if (threadIdx.x == 0) finish(A, row, lse, xt);
   if (A.logprobs) P.write(A.logprobs + row * A.out_stride, lse);
 }
 
@@ -347,8 +348,8 @@ __global__ __launch_bounds__(256) void k_logits_join(LogitArgs A, int32_t slots)
   const float k = kLog2e / A.r.temperature;
   for (int32_t i = threadIdx.x; i < A.splits; i += 256) join(s, A.part[2 * (row * A.splits + i)], A.part[2 * (row * A.splits + i) + 1], k);
   s = block_sum(s, k);
-  const Lse lse = log_sum(s);
-  if (part == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row], k);
+  const Lse lse = log_sum(s, A.r.temperature);
+  if (part == 0 && threadIdx.x == 0) finish(A, row, lse, A.part[2 * A.rows * A.splits + row]);
   if (!A.logprobs) return;
   Part<T> P;
   P.start(A, row, part, A.splits, slots, shared);
@@ -456,21 +457,21 @@ __global__ __launch_bounds__(256) void k_logits_short(LogitArgs A) {
 #pragma unroll
     for (int e = 0; e < E; ++e) s.l += term(x[e], base, k);
     s.l = over_lanes<L>(s.l, Plus());
-    const Lse lse = log_sum(s);
+    const Lse lse = log_sum(s, A.r.temperature);
     if (!live) continue;
-    if (A.lse && lane == 0) A.lse[row] = lse.value(A.r.temperature);
+    if (A.lse && lane == 0) A.lse[row] = lse.value();
     if (A.score) {
       const int32_t t = A.target[row];
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (lane + L * e == t && t < A.classes) A.score[row] = log_prob(x[e], k, lse);
+        if (lane + L * e == t && t < A.classes) A.score[row] = log_prob(x[e], lse);
       if (lane == 0 && (t < 0 || t >= A.classes)) A.score[row] = t < 0 ? 0.0f : __builtin_nanf("");
     }
     if (A.logprobs) {
       float* dst = A.logprobs + row * A.out_stride;
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        if (lane + L * e < A.classes) dst[lane + L * e] = log_prob(x[e], k, lse);
+        if (lane + L * e < A.classes) dst[lane + L * e] = log_prob(x[e], lse);
     }
   }
 }

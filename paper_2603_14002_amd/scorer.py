@@ -4,12 +4,17 @@ the C ABI, over torch tensors.
 The functions check what the C side cannot see of a tensor (its type, shape, device and
 layout), raise ``LBError`` for it as for the library's own refusals, allocate the outputs
 and workspaces that are not given, and enqueue the call on ``stream`` (None: torch's
-current stream of the tensors' device).  Every step runs in the library's HIP kernels.
+current stream of the tensors' device).  Every step runs in the library's HIP kernels, and
+no gradients are recorded.
+
+A call on few rows is mostly this file's work, so what a function has made itself is not
+checked again, and nothing that the common case does not need is called.
 """
 
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional
 
 LB_F32, LB_BF16, LB_F16 = 0, 1, 2
@@ -234,20 +239,24 @@ class KVBatch:
     [n_seqs] and pages [n_seqs, max_pages]; `n_rows` rows of activations, at most `max_new`
     new tokens a sequence.  The tensors may be changed between calls."""
 
-    __slots__ = ("starts", "lengths", "pages", "n_rows", "device", "desc", "ref")
+    __slots__ = ("starts", "lengths", "pages", "n_rows", "max_pages", "device", "desc", "ref")
 
     def __init__(self, starts, lengths, pages, n_rows: int, max_new: int):
         if torch is None:
             _load()
-        n = lengths.shape[0] if lengths.dim() else 0
-        _ints(starts, "starts", (n + 1,))
-        _ints(lengths, "lengths", (n,))
-        _ints(pages, "the page table", (n, None))
-        self.device = starts.get_device()
-        if lengths.get_device() != self.device or pages.get_device() != self.device:
-            _elsewhere(self.device, lengths=lengths, pages=pages)
-        self.starts, self.lengths, self.pages, self.n_rows = starts, lengths, pages, n_rows
-        self.desc = lb_kv_batch(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), n, n_rows, pages.shape[1], max_new)
+        i32, at = torch.int32, pages.shape
+        n = at[0] if len(at) == 2 else -1
+        if starts.dtype is not i32 or lengths.dtype is not i32 or pages.dtype is not i32 or starts.shape != (n + 1,) or lengths.shape != (n,) \
+                or not starts.is_contiguous() or not lengths.is_contiguous() or not pages.is_contiguous():
+            n = lengths.shape[0] if lengths.dim() else 0
+            _ints(starts, "starts", (n + 1,))
+            _ints(lengths, "lengths", (n,))
+            _ints(pages, "the page table", (n, None))
+        self.device = g = starts.get_device()
+        if lengths.get_device() != g or pages.get_device() != g:
+            _elsewhere(g, lengths=lengths, pages=pages)
+        self.starts, self.lengths, self.pages, self.n_rows, self.max_pages = starts, lengths, pages, n_rows, at[1]
+        self.desc = lb_kv_batch(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), n, n_rows, at[1], max_new)
         self.ref = ctypes.addressof(self.desc)
 
 
@@ -328,11 +337,12 @@ def lb_kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope: Optional[Rope] =
     hq = qs = os = 0
     if q is not None:
         qs, hq = _heads(q, "q", n, None, D, dtype), q.shape[1]
-        if q_out is None:
-            q_out = _empty((n, hq, D), dtype, q, stream)
-        os = _heads(q_out, "q_out", n, hq, D, dtype)
-        if q.get_device() != g or q_out.get_device() != g:
+        if q.get_device() != g or (q_out is not None and q_out.get_device() != g):
             _elsewhere(g, q=q, q_out=q_out)
+        if q_out is None:
+            q_out, os = _empty((n, hq, D), dtype, q, stream), hq * D
+        else:
+            os = _heads(q_out, "q_out", n, hq, D, dtype)
     elif q_out is not None:
         _bad("q_out needs q")
     _call(g, stream, "lb_kv_append", cache.ref, batch.ref, None if rope is None else rope.ref, dt, hq, _ptr(q), qs,
@@ -347,11 +357,19 @@ def lb_kv_read(cache: KVCache, batch: KVBatch, dtype=None, k_out=None, v_out=Non
     if dtype is None:
         given = k_out if k_out is not None else v_out
         dtype = torch.float32 if given is None else given.dtype
-    k_out = _empty((n, H, D), dtype, cache.pages, stream) if k_out is None else k_out
-    v_out = _empty((n, H, D), dtype, cache.pages, stream) if v_out is None else v_out
-    ks, vs = _heads(k_out, "k_out", n, H, D, dtype), _heads(v_out, "v_out", n, H, D, dtype)
-    if batch.device != g or k_out.get_device() != g or v_out.get_device() != g:
-        _elsewhere(g, starts=batch.starts, k_out=k_out, v_out=v_out)
+    ks = vs = H * D
+    if batch.device != g:
+        _elsewhere(g, starts=batch.starts)
+    if k_out is None:
+        k_out = _empty((n, H, D), dtype, cache.pages, stream)
+    else:
+        ks = _heads(k_out, "k_out", n, H, D, dtype)
+        _elsewhere(g, k_out=k_out)
+    if v_out is None:
+        v_out = _empty((n, H, D), dtype, cache.pages, stream)
+    else:
+        vs = _heads(v_out, "v_out", n, H, D, dtype)
+        _elsewhere(g, v_out=v_out)
     _call(g, stream, "lb_kv_read", cache.ref, batch.ref, _dtype(k_out, "k_out"), k_out.data_ptr(), ks, v_out.data_ptr(), vs)
     return k_out, v_out
 
@@ -369,21 +387,28 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
     dt, dtype, n, D, g = _dtype(q, "q"), q.dtype, batch.n_rows, cache.head_dim, cache.device
     qs = _heads(q, "q", n, None, D, dtype)
     hq = q.shape[1]
+    if batch.device != g or q.get_device() != g:
+        _elsewhere(g, starts=batch.starts, q=q)
     if out is None:
-        out = _empty((n, hq, D), dtype, q, stream)
-    os = _heads(out, "out", n, hq, D, dtype)
-    if lse is None and want_lse:
+        out, os = _empty((n, hq, D), dtype, q, stream), hq * D
+    else:
+        os = _heads(out, "out", n, hq, D, dtype)
+        _elsewhere(g, out=out)
+    if lse is not None:
+        if lse.dtype is not torch.float32 or lse.shape != (n, hq) or not lse.is_contiguous():
+            _bad(f"lse must be contiguous float32 ({n}, {hq})")
+        _elsewhere(g, lse=lse)
+    elif want_lse:
         lse = _empty((n, hq), torch.float32, q, stream)
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (n, hq) or not lse.is_contiguous()):
-        _bad(f"lse must be contiguous float32 ({n}, {hq})")
-    if batch.device != g or q.get_device() != g or out.get_device() != g or (lse is not None and lse.get_device() != g):
-        _elsewhere(g, starts=batch.starts, q=q, out=out, lse=lse)
-    ws, nbytes, _held = _scratch(q, stream, 0 if workspace is not None else lb_kv_attend_workspace(cache, batch, hq), workspace, "lb_kv_attend")
+    ws, nbytes, _held = None, 0, None
+    if workspace is not None or batch.max_pages * cache.page_tokens >= 1024:  # shorter key ranges have no parts, and need none
+        ws, nbytes, _held = _scratch(q, stream, 0 if workspace is not None else lb_kv_attend_workspace(cache, batch, hq), workspace, "lb_kv_attend")
     _call(g, stream, "lb_kv_attend", cache.ref, batch.ref, dt, hq, q.data_ptr(), qs, scale, window, out.data_ptr(), os,
           _ptr(lse), ws, nbytes)
     return out, lse
 
 
+@functools.lru_cache(maxsize=4096)
 def lb_lora_workspace(rows: int, d_in: int, d_out: int, rank: int) -> int:
     _load()
     need = _L()
@@ -420,6 +445,7 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def lb_logits_workspace(rows: int, classes: int) -> int:
     _load()
     need = _L()

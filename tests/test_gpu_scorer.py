@@ -359,6 +359,32 @@ def test_attend_rows_that_see_nothing():
     close(lse[1:2], wl, bl, "lse")
 
 
+def test_thousands_of_ragged_sequences():
+    """Each workgroup finds its sequence among 5000 of 0 to 5 new tokens: appended blocks, what is read back, and
+    attention by both kernels (5 tokens of 16 heads are many rows, fewer are few)."""
+    rng = np.random.default_rng(17)
+    new = [int(x) for x in rng.integers(0, 6, 5000)]
+    length = [n + int(x) for n, x in zip(new, rng.integers(0, 20, 5000))]
+    R = ref.Ragged(new, length, 16, 1, 64, seed=18)
+    rows, n = R.rows(), R.n_rows
+    k, v = randn(rng, n, 1, 64, dtype=torch.bfloat16), randn(rng, n, 1, 64, dtype=torch.bfloat16)
+    # the tokens before the new ones: the same for all
+    old = [randn(rng, 20, 1, 64, dtype=torch.float64) for _ in range(2)]
+    for s, (m, ln) in enumerate(zip(new, length)):
+        R.put(s, old[0][:ln - m], old[1][:ln - m])
+    cache, batch = handles(R)
+    say("[case] thousands")
+    lbm.lb_kv_append(cache, batch, None, dev(k), dev(v))
+    kr, vr = lbm.lb_kv_read(cache, batch)
+    for got, x in ((kr, k), (vr, v)):
+        assert torch.equal(got.cpu().double(), ref.decode(*ref.encode(x)))
+    q = dev(randn(rng, n, 16, 64, dtype=torch.bfloat16))
+    out, lse = lbm.lb_kv_attend(cache, batch, q, 0.125, want_lse=True)
+    assert cache.status() == 0 and n * 16 >= 128 * 600 and max(new) == 5
+    R.pages = cache.pages.cpu()
+    check_attend(R, q, out, lse, 0.125, 0, skip=set(range(5000)) - set(range(0, 5000, 7)) - set(range(4900, 5000)))
+
+
 def test_attend_leaves_rows_out_that_no_sequence_has():
     """Starts that do not fit: the rows between the sequences, and those past max_new, stay as they were, with one
     part of the keys and with several."""
