@@ -1034,7 +1034,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(Atten
 // from memory.  A ring of 2 A tiles has a barrier every A tiles: at step t the keys
 // of t + 1 and the values of t are read, made A steps or more before, and those of t
 // + 1 + A and t + A are made, in places that were last read A steps or more before.
-// Six prompts of 65..2048 tokens over 130..4096, 32 heads of 128 on 8, bf16: 343 us,
+// Six prompts of 65..2048 tokens over 130..4096, 32 heads of 128 on 8, bf16: 341 us,
 // 680 TFLOP/s; vector instructions are issued in half of the SIMD cycles (a lane's
 // eight scores of a row take 8 products, exponentials and sums each), matrix ones run
 // in 29 %, and two wavefronts a SIMD do not cover each other's waits.

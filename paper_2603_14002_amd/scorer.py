@@ -288,25 +288,33 @@ class LogitRules:
         if torch is None:
             _load()
         self.history, self.bias_ids, self.bias_values, self.mask, self.mask_row = history, bias_ids, bias_values, mask, mask_row
+        i32 = torch.int32
         h = bi = bv = mk = mr = None
         hw = bw = per_row = masks = 0
         if history is not None:
-            _ints(history, "history", (None, None))
-            h, hw = history.data_ptr(), history.shape[1]
+            at = history.shape
+            if history.dtype is not i32 or len(at) != 2 or not history.is_contiguous():
+                _ints(history, "history", (None, None))
+            h, hw = history.data_ptr(), at[1]
         if (bias_ids is None) != (bias_values is None):
             _bad("bias_ids and bias_values belong together")
         if bias_ids is not None:
-            _ints(bias_ids, "bias_ids", (None, None))
-            if bias_values.dtype is not torch.float32 or bias_values.shape != bias_ids.shape or not bias_values.is_contiguous():
+            at = bias_ids.shape
+            if bias_ids.dtype is not i32 or len(at) != 2 or not bias_ids.is_contiguous():
+                _ints(bias_ids, "bias_ids", (None, None))
+            if bias_values.dtype is not torch.float32 or bias_values.shape != at or not bias_values.is_contiguous():
                 _bad("bias_values must be contiguous float32 of bias_ids' shape")
-            bi, bv, bw, per_row = bias_ids.data_ptr(), bias_values.data_ptr(), bias_ids.shape[1], int(bias_ids.shape[0] != 1)
+            bi, bv, bw, per_row = bias_ids.data_ptr(), bias_values.data_ptr(), at[1], 0 if at[0] == 1 else 1
         if mask is not None:
-            _ints(mask, "mask", (None, None))
-            mk, masks = mask.data_ptr(), mask.shape[0]
+            at = mask.shape
+            if mask.dtype is not i32 or len(at) != 2 or not mask.is_contiguous():
+                _ints(mask, "mask", (None, None))
+            mk, masks = mask.data_ptr(), at[0]
         if mask_row is not None:
             if mask is None:
                 _bad("mask_row needs a mask")
-            _ints(mask_row, "mask_row", (None,))
+            if mask_row.dtype is not i32 or len(mask_row.shape) != 1 or not mask_row.is_contiguous():
+                _ints(mask_row, "mask_row", (None,))
             mr = mask_row.data_ptr()
         self.desc = lb_logit_rules(temperature, repetition, presence, frequency, h, bi, bv, mk, mr, hw, bw, per_row, masks)
         self.ref = ctypes.addressof(self.desc)
