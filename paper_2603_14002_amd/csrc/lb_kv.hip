@@ -960,7 +960,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend_short
 // Few query rows: a workgroup takes 16 rows and one part of their key range; its
 // four wavefronts take every fourth tile and join at the end.  once: nobody else
 // reads the keys, which then leave the caches to others (4 x 110 000 keys of 8 heads:
-// 88 us, else 98).
+// 89 us, else 99).
 template <int D, typename T, bool once>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
@@ -1338,7 +1338,7 @@ constexpr int64_t kLeastGroups = 600;  // of 128 rows
 // How a call is cut up.  Sequences with at most few_rows query rows a KV head: tiles
 // of 16 rows, and parts of the key range so that about three workgroups a CU exist
 // (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8 heads
-// take 99 us with them, 101 with six, 106 with eight), each with 16 tiles of keys at
+// take 89 us with them, 102 with two, 92 with six, 97 with eight), each with 16 tiles of keys at
 // least; where there are many such jobs with at most 16 tiles of keys, a wavefront
 // takes one alone (1024 sequences of 3 to 256 keys, 4 heads of 64: 16 us, else 26).
 // The others: a workgroup takes the rows of its four wavefronts, and the workgroups
