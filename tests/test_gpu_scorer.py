@@ -853,3 +853,66 @@ def test_cached_lm_answers_a_request():
             m = int(counts[at])
             want = lm64(lm, cached, (-1, tuple(words[at][:m].tolist())))[0] if m > 0 else 0.0
             assert abs(float(got[at]) - want) <= max(m, 0) * 64 * d * 2.0 ** -24
+
+
+def _three(seed):
+    """Inputs of calls that need workspaces, and the calls with all memory their own."""
+    rng = np.random.default_rng(seed)
+    R = ref.Ragged([1, 2], [1900, 1400], 16, 2, 64, seed=seed)
+    for s, ln in enumerate(R.length):
+        R.put(s, randn(rng, ln, 2, 64, dtype=torch.float64), randn(rng, ln, 2, 64, dtype=torch.float64))
+    cache, batch = handles(R)
+    q, logits = dev(randn(rng, 3, 8, 64)), dev(randn(rng, 2, 30000))
+    x, y = dev(randn(rng, 300, 64)), dev(randn(rng, 300, 96))
+    a, b = dev(randn(rng, 4, 16, 64)), dev(randn(rng, 4, 96, 16))
+    ids = dev(torch.arange(300, dtype=torch.int32) % 5)
+    target = dev(torch.tensor([3, 29999], dtype=torch.int32))
+
+    def calls(stream=None):
+        out, lse = lbm.lb_kv_attend(cache, batch, q, 0.2, want_lse=True, stream=stream)
+        z = lbm.lb_lora_add(y, x, a, b, ids, out=torch.empty_like(y), stream=stream)
+        return [out, lse, z, *lbm.lb_logits_adjust(logits, target=target, stream=stream)]
+
+    assert lbm.lb_kv_attend_workspace(cache, batch, 8) > 0 and lbm.lb_lora_workspace(300, 64, 96, 16) > 0 \
+        and lbm.lb_logits_workspace(2, 30000) > 0
+    return calls, [q, x, logits]
+
+
+def test_captured_calls_with_workspaces_of_their_own():
+    calls, ins = _three(30)
+    say("[case] graph, own workspaces")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = calls()
+    for k in range(4):
+        for t in ins:
+            t.mul_(-0.75 if k % 2 else 1.25)
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in got]
+        for a, b in zip(replayed, calls()):
+            assert torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each has outputs and workspaces of its own: the results are those of one after the other."""
+    sets = [_three(31), _three(32)]
+    want = [[t.clone() for t in calls()] for calls, _ in sets]
+    torch.cuda.synchronize()
+    say("[case] two streams at once")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(10):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                got.append((k, sets[k][0]()))
+    torch.cuda.synchronize()
+    for k, outs in got:
+        for a, b in zip(outs, want[k]):
+            assert torch.equal(a, b)
