@@ -426,38 +426,39 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs A) {
 // lanes until the end.
 //
 // Scores, maxima, sums and outputs are held in 32 bits.  The matrix operands are
-// bf16: keys and values exactly; queries and probabilities in `NP` pieces, each
-// the rounding of what the ones before leave: one piece (off by at most 2^-8 of a
-// probability) for bf16, whose output has that rounding anyway, two (2^-16) for
-// fp16, three (2^-24) for fp32.  bf16 queries are exact with one, fp16 ones with two.
+// bf16: keys and values exactly; queries and probabilities in pieces, each the
+// rounding of what the ones before leave.  Queries are exact: one piece for bf16,
+// two for fp16, three for fp32.  Probabilities have two for bf16 and fp16 (off by at
+// most 2^-16 of a probability: with one, 2^-8, an output would be off by as much
+// again as by its own rounding to bf16) and three for fp32 (2^-24).
 
 template <typename T>
 struct Pieces;
 template <>
 struct Pieces<__bf16> {
-  static constexpr int n = 1;
+  static constexpr int q = 1, p = 2;
 };
 template <>
 struct Pieces<_Float16> {
-  static constexpr int n = 2;
+  static constexpr int q = 2, p = 2;
 };
 template <>
 struct Pieces<float> {
-  static constexpr int n = 3;
+  static constexpr int q = 3, p = 3;
 };
 
-template <int NP>
-__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&w)[NP]) {
+// inf: some x may be infinite.  It is one piece: the rest of it would be NaN.
+template <bool inf, int N>
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&w)[N]) {
   float rest[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) rest[i] = x[i];
 #pragma unroll
-  for (int k = 0; k < NP; ++k)
+  for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       w[k][i] = static_cast<__bf16>(rest[i]);
-      // an infinity is one piece: the rest of it would be NaN
-      if (k + 1 < NP) rest[i] = __builtin_isinf(rest[i]) ? 0.0f : rest[i] - static_cast<float>(w[k][i]);
+      if (k + 1 < N) rest[i] = inf && __builtin_isinf(rest[i]) ? 0.0f : rest[i] - static_cast<float>(w[k][i]);
     }
 }
 
@@ -666,10 +667,10 @@ __device__ __forceinline__ bf16x8 channel(const uint32_t (&y)[2][4], int odd) {
 }
 
 // The state of QT tiles of 16 query rows in one wavefront.
-template <int D, int NP, int QT>
+template <int D, typename T, int QT>
 struct Rows {
-  static constexpr int KC = D / 32, VC = D / 16;
-  bf16x8 q[QT][KC][NP];
+  static constexpr int KC = D / 32, VC = D / 16, NQ = Pieces<T>::q, NP = Pieces<T>::p;
+  bf16x8 q[QT][KC][NQ];
   f32x4 o[QT][VC];
   float m[QT], l[QT];  // reference and the lane's share of the sum of exp2(score - reference)
   int32_t pos[QT];     // the lane's row's position, -1: no row
@@ -699,7 +700,7 @@ struct Rows {
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
-          for (int p = 0; p < NP; ++p) acc[t][u] = mfma(kf, q[t][c][p], acc[t][u]);
+          for (int p = 0; p < NQ; ++p) acc[t][u] = mfma(kf, q[t][c][p], acc[t][u]);
       }
     }
   }
@@ -747,7 +748,7 @@ struct Rows {
         p[i] = __builtin_amdgcn_exp2f(fmaf(acc[t][i >> 2][i & 3], scale2, -base));
         l[t] += p[i];
       }
-      split8<NP>(p, pf[t]);
+      split8<false>(p, pf[t]);  // no score passes the reference by more than kSlack
     }
   }
 
@@ -831,7 +832,7 @@ struct Rows {
 };
 
 // Wavefronts a SIMD that the registers are bounded for: as many as go without
-// spilling (o and q take 4 D/16 + 4 D/32 NP registers a row tile).
+// spilling (o and q take 4 D/16 + 4 D/32 NQ registers a row tile; pieces: of the query).
 constexpr int waves(int D, int pieces, int QT) { return D * QT * (1 + pieces) <= 256 ? 3 : D * QT * (1 + pieces) <= 768 ? 2 : 1; }
 
 constexpr int kMostSplits = 128;  // parts of a key range
@@ -866,7 +867,7 @@ __device__ __forceinline__ void report(const AttendArgs& A, const Job& w) {
 
 // Rows r0 .. r0 + 16 QT - 1 of the job into a wavefront's state; false: there are none.
 template <int D, typename T, int QT>
-__device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32_t r0, Rows<D, Pieces<T>::n, QT>& S, int n, int j) {
+__device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32_t r0, Rows<D, T, QT>& S, int n, int j) {
   S.scale2 = fabsf(A.scale2);
   float sign = A.scale2 < 0.0f ? -1.0f : 1.0f;
   if (A.scale2 == 0.0f) sign = 0.0f, S.scale2 = 1.0f;
@@ -891,7 +892,7 @@ __device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32
       if (live) load8(static_cast<const T*>(A.q) + (w.q.row0 + static_cast<int64_t>(i)) * A.q_stride + (w.h * w.G + g) * D + j * (D / 4) + c * 8, x);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[k] *= sign;
-      split8<Pieces<T>::n>(x, S.q[t][c]);
+      split8<true>(x, S.q[t][c]);
     }
   }
   return have;
@@ -920,7 +921,7 @@ __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -
 
 // The results of a wavefront's rows r0 .. r0 + 16 QT - 1 that have seen all of their keys.
 template <int D, typename T, int QT>
-__device__ __forceinline__ void store_rows(const AttendArgs& A, const Job& w, int32_t r0, const Rows<D, Pieces<T>::n, QT>& S, int n, int j) {
+__device__ __forceinline__ void store_rows(const AttendArgs& A, const Job& w, int32_t r0, const Rows<D, T, QT>& S, int n, int j) {
   constexpr int VC = D / 16;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -943,13 +944,13 @@ __device__ __forceinline__ void store_rows(const AttendArgs& A, const Job& w, in
 // Few query rows and short key ranges, but many of them: a wavefront takes a job on
 // its own, and has nothing to join.
 template <int D, typename T>
-__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend_short(AttendArgs A) {
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend_short(AttendArgs A) {
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const uint32_t job = blockIdx.x * 4 + wave_index();
   if (job >= static_cast<uint32_t>(A.kv.n_seqs * A.tiles * A.kv.kv_heads)) return;
   const Job w = few_job(A, job);
   if (lane == 0) report(A, w);
-  Rows<D, Pieces<T>::n, 1> S;
+  Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
   Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
@@ -962,14 +963,14 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend_short
 // reads the keys, which then leave the caches to others (4 x 110 000 keys of 8 heads:
 // 89 us, else 99).
 template <int D, typename T, bool once>
-__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, 1)) void k_attend(AttendArgs A) {
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   const uint32_t job = blockIdx.x / A.splits;
   const int32_t split = static_cast<int32_t>(blockIdx.x % A.splits);
   const Job w = few_job(A, job);
   if (split == 0 && threadIdx.x == 0) report(A, w);
-  Rows<D, Pieces<T>::n, 1> S;
+  Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
   const int32_t tiles = S.end > begin ? (S.end - begin + 31) >> 5 : 0;
@@ -1129,15 +1130,16 @@ struct Maker {
 };
 
 // Operands that the many-row kernel reads ahead: as many of N as the registers hold beside its state.
-constexpr int ahead(int D, int pieces, int QT, int N) {
-  const int state = 4 * QT * (D / 16 + D / 32 * pieces + 2 + pieces) + 56, room = (256 - state) / 8;
+template <int D, typename T, int QT>
+constexpr int ahead(int N) {
+  const int state = 4 * QT * (D / 16 + D / 32 * Pieces<T>::q + 2 + Pieces<T>::p) + 56, room = (256 - state) / 8;
   return room >= N ? N : room >= N / 2 ? N / 2 : room >= 4 ? 4 : 2;
 }
 
 template <int D, typename T, int QT>
-__global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows(AttendArgs A) {
-  constexpr int KC = D / 32, VC = D / 16, NP = Pieces<T>::n, per = 64 * QT;
-  constexpr int KA = ahead(D, NP, QT, 2 * KC), VA = ahead(D, NP, QT, VC);
+__global__ __launch_bounds__(256, waves(D, Pieces<T>::q, QT)) void k_attend_rows(AttendArgs A) {
+  constexpr int KC = D / 32, VC = D / 16, NP = Pieces<T>::p, per = 64 * QT;
+  constexpr int KA = ahead<D, T, QT>(2 * KC), VA = ahead<D, T, QT>(VC);
   __shared__ Shared<D> L;
   const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, j = lane >> 4;
   if (A.few_rows == 0) check_sequence(A.kv, blockIdx.x);
@@ -1152,7 +1154,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::n, QT)) void k_attend_rows
   if (w.tile < 0 || w.tile >= tiles_of_rows) return;
   w.tile = tiles_of_rows - 1 - w.tile;  // the last rows see most keys: they go first
   // a wavefront without rows goes along, and sees nothing
-  Rows<D, NP, QT> S;
+  Rows<D, T, QT> S;
   const bool have = rows_of<D, T, QT>(A, w, (w.tile * 4 + wave) * 16 * QT, S, n, j);
   // the key range of all four wavefronts' rows
   const int32_t first = w.q.pos0 + w.tile * per / w.G, last = w.q.pos0 + (min(w.R, (w.tile + 1) * per) - 1) / w.G;
@@ -1298,7 +1300,7 @@ template <int D, typename T>
 hipError_t attend(const AttendArgs& A, hipStream_t st) {
   if (A.units) {
     const int64_t blocks = A.units * A.kv.kv_heads;
-    k_attend_rows<D, T, row_tiles(D, Pieces<T>::n)><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
+    k_attend_rows<D, T, row_tiles(D, Pieces<T>::q)><<<dim3(static_cast<unsigned>(blocks)), 256, 0, st>>>(A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.few_rows == 0) return e;
   }
@@ -1353,7 +1355,8 @@ constexpr int64_t kLeastGroups = 600;  // of 128 rows
 AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   AttendPlan p{};
   const int64_t G = kv.q_heads / kv.kv_heads, rows = kv.max_new * G;
-  const int64_t units = kv.n_rows * G / (4 * 16 * row_tiles(head_dim, dtype == LB_BF16 ? 1 : dtype == LB_F16 ? 2 : 3)) + kv.n_seqs;
+  const int pieces = dtype == LB_BF16 ? Pieces<__bf16>::q : dtype == LB_F16 ? Pieces<_Float16>::q : Pieces<float>::q;
+  const int64_t units = kv.n_rows * G / (4 * 16 * row_tiles(head_dim, pieces)) + kv.n_seqs;
   p.splits = 1;
   p.few_rows = 0x7FFFFFFF;
   if (rows > 64 && kv.n_rows * G * kv.kv_heads >= 128 * kLeastGroups) {
