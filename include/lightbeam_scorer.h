@@ -91,8 +91,9 @@ typedef struct lb_kv_batch {
   int32_t max_new;        /* at least every sequence's number of new tokens     */
 } lb_kv_batch;
 /* (max_pages * page_tokens is at most 2^30.  A call's workgroups number less than
- * 2^24: lb_kv_attend refuses batches that need more, about 2^30 query rows and
- * heads.) */
+ * 2^24: lb_kv_attend and lb_kv_attend_workspace refuse batches that need more.  They
+ * take every batch with kv_heads * (n_seqs + n_rows * (q_heads / kv_heads) / 16)
+ * below that, whatever max_new is.) */
 
 /* Rotation of keys and queries: with row p of the tables for position p, the
  * pair (x1, x2) of channels becomes (x1 cos - x2 sin, x2 cos + x1 sin); pair i

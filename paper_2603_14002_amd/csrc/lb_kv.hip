@@ -847,22 +847,34 @@ struct Job {
   int32_t s, h, tile, G, R;
 };
 
-// The job of the few-row kernel: tile `rest % tiles` of head h of sequence s.
+// A job of the few-row kernel, numbered by `tiles` tiles to every sequence and head,
+// or, with few_units, as the many-row kernel's units are.
 __device__ __forceinline__ Job few_job(const AttendArgs& A, uint32_t job) {
   Job w;
-  w.tile = static_cast<int32_t>(job % A.tiles);
-  job /= A.tiles;
-  w.h = static_cast<int32_t>(job % A.kv.kv_heads);
-  w.s = static_cast<int32_t>(job / A.kv.kv_heads);
-  w.q = sequence(A.kv, w.s);
   w.G = A.kv.q_heads / A.kv.kv_heads;
+  if (A.few_units) {
+    w.h = static_cast<int32_t>(job % A.kv.kv_heads);
+    w.s = row_unit(A.kv, static_cast<int32_t>(job / A.kv.kv_heads), w.G, 16, &w.tile);
+  } else {
+    w.tile = static_cast<int32_t>(job % A.tiles);
+    job /= A.tiles;
+    w.h = static_cast<int32_t>(job % A.kv.kv_heads);
+    w.s = static_cast<int32_t>(job / A.kv.kv_heads);
+  }
+  w.q = sequence(A.kv, w.s);
   w.R = w.q.count * w.G;
   if (w.R > A.few_rows) w.R = 0;  // the many-row kernel's
+  if (A.few_units && (w.tile < 0 || w.tile >= (w.R + 15) >> 4)) w.R = w.tile = 0;
   return w;
 }
-// every sequence has a job of tile 0 and head 0
-__device__ __forceinline__ void report(const AttendArgs& A, const Job& w) {
-  if (w.q.bad && w.tile == 0 && w.h == 0) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+// By one lane: every sequence has a job of tile 0 and head 0, or a unit of its number.
+__device__ __forceinline__ void report(const AttendArgs& A, const Job& w, uint32_t job) {
+  if (A.few_units) {
+    const uint32_t s = job / A.kv.kv_heads;
+    if (s < static_cast<uint32_t>(A.kv.n_seqs) && w.h == 0 && sequence(A.kv, static_cast<int32_t>(s)).bad) raise(A.kv.flags, LB_KV_BAD_LENGTH);
+  } else if (w.q.bad && w.tile == 0 && w.h == 0) {
+    raise(A.kv.flags, LB_KV_BAD_LENGTH);
+  }
 }
 
 // Rows r0 .. r0 + 16 QT - 1 of the job into a wavefront's state; false: there are none.
@@ -947,9 +959,9 @@ template <int D, typename T>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend_short(AttendArgs A) {
   const int lane = threadIdx.x & 63, n = lane & 15, j = lane >> 4;
   const uint32_t job = blockIdx.x * 4 + wave_index();
-  if (job >= static_cast<uint32_t>(A.kv.n_seqs * A.tiles * A.kv.kv_heads)) return;
+  if (job >= A.jobs) return;
   const Job w = few_job(A, job);
-  if (lane == 0) report(A, w);
+  if (lane == 0) report(A, w, job);
   Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
@@ -969,7 +981,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend(Atten
   const uint32_t job = blockIdx.x / A.splits;
   const int32_t split = static_cast<int32_t>(blockIdx.x % A.splits);
   const Job w = few_job(A, job);
-  if (split == 0 && threadIdx.x == 0) report(A, w);
+  if (split == 0 && threadIdx.x == 0) report(A, w, job);
   Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
   const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
@@ -1304,7 +1316,7 @@ hipError_t attend(const AttendArgs& A, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || A.few_rows == 0) return e;
   }
-  const int64_t jobs = static_cast<int64_t>(A.kv.n_seqs) * A.tiles * A.kv.kv_heads;
+  const int64_t jobs = A.jobs;
   if (A.alone) {
     k_attend_short<D, T><<<dim3(static_cast<unsigned>((jobs + 3) / 4)), 256, 0, st>>>(A);
     return hipGetLastError();
@@ -1338,7 +1350,9 @@ hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStr
 constexpr int64_t kLeastGroups = 600;  // of 128 rows
 
 // How a call is cut up.  Sequences with at most few_rows query rows a KV head: tiles
-// of 16 rows, and parts of the key range so that about three workgroups a CU exist
+// of 16 rows, as many for each as max_new may need or, where those are more, numbered
+// by the rows there are (1024 single tokens beside a prompt of 500, 32 heads of 128 on
+// 8, bf16: 110 us, else 1462; two sequences of up to 100 new tokens: 8.0, else 7.6), and parts of the key range so that about three workgroups a CU exist
 // (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8 heads
 // take 89 us with them, 102 with two, 92 with six, 97 with eight), each with 16 tiles of keys at
 // least; where there are many such jobs with at most 16 tiles of keys, a wavefront
@@ -1357,22 +1371,28 @@ AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   const int64_t G = kv.q_heads / kv.kv_heads, rows = kv.max_new * G;
   const int pieces = dtype == LB_BF16 ? Pieces<__bf16>::q : dtype == LB_F16 ? Pieces<_Float16>::q : Pieces<float>::q;
   const int64_t units = kv.n_rows * G / (4 * 16 * row_tiles(head_dim, pieces)) + kv.n_seqs;
+  const int64_t most_units = kv.n_rows * G / (4 * 16 * row_tiles(head_dim, Pieces<float>::q)) + kv.n_seqs;
   p.splits = 1;
   p.few_rows = 0x7FFFFFFF;
   if (rows > 64 && kv.n_rows * G * kv.kv_heads >= 128 * kLeastGroups) {
     p.units = units;
+    p.groups = most_units * kv.kv_heads;
     p.few_rows = kv.n_seqs == 1 ? 0 : 64;
     if (p.few_rows == 0) return p;
   }
   const int64_t most = rows < p.few_rows ? rows : p.few_rows;
   p.tiles = static_cast<int32_t>((most + 15) / 16);
   p.part_rows = static_cast<int32_t>(most < 16 ? most : 16);
-  const int64_t jobs = static_cast<int64_t>(kv.n_seqs) * p.tiles * kv.kv_heads;
+  const int64_t few_units = kv.n_rows * G / 16 + kv.n_seqs;
+  const bool numbered = few_units < static_cast<int64_t>(kv.n_seqs) * p.tiles;
+  p.few_units = numbered ? few_units : 0;
+  const int64_t jobs = p.jobs = (numbered ? few_units : static_cast<int64_t>(kv.n_seqs) * p.tiles) * kv.kv_heads;
   const int64_t tokens = static_cast<int64_t>(kv.max_pages) << kv.page_shift;
   p.alone = tokens <= 512 && jobs > 2048;
   int64_t s = (768 + jobs - 1) / jobs;
   s = s < tokens / 512 ? s : tokens / 512;
   p.splits = static_cast<int32_t>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
+  p.groups = p.groups > jobs * p.splits ? p.groups : jobs * p.splits;
   if (p.splits > 1) {
     p.part_sums = jobs * p.part_rows * p.splits * head_dim;
     p.part_floats = p.part_sums + jobs * p.part_rows * p.splits * 2;

@@ -48,6 +48,7 @@ struct AttendArgs {
   int32_t window;
   // the plan's
   int32_t tiles, splits, part_rows;
+  uint32_t few_units, jobs;
   int64_t units, part_sums;
   int32_t few_rows;
   bool alone;
@@ -77,16 +78,19 @@ struct LogitArgs {
 
 // How an attention call is cut up (see attend_plan).  Few-row kernel: the query rows
 // of a sequence and KV head up to which it takes them (0: it does not run), tiles of
-// 16 rows, whether a wavefront takes one alone, the parts that a key range is cut
+// 16 rows, their units if they are numbered by the rows there are (else 0), jobs in
+// all, whether a wavefront takes one alone, the parts that a key range is cut
 // into, the rows of a tile whose parts are kept, the floats of these and where the
-// parts' sums start among them.  Many-row kernel: its units of rows, 0: none.
+// parts' sums start among them.  Many-row kernel: its units of rows, 0: none.  groups:
+// the most workgroups that a launch would have, of any type.
 struct AttendPlan {
   int32_t few_rows;
   bool alone;
   int32_t tiles, splits, part_rows;
-  int64_t part_floats, part_sums, units;
+  int64_t few_units, jobs;
+  int64_t part_floats, part_sums, units, groups;
 };
-AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype);  // part_floats is the same for every type
+AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype);  // part_floats and groups are the same for every type
 
 hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st);

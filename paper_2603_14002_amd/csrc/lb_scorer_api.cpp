@@ -110,6 +110,13 @@ void check_heads(const KvArgs& a) {
        "max_new * q_heads / kv_heads must be at most 2^30");
 }
 
+// the plan of a call that launches can take
+AttendPlan checked_plan(const KvArgs& a, int32_t head_dim, int32_t dtype) {
+  const AttendPlan p = attend_plan(a, head_dim, dtype);
+  need(p.groups <= kMostGroups, "too much work for one call: n_seqs or n_rows * q_heads is too large");
+  return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -207,7 +214,7 @@ lb_status lb_kv_attend_workspace(const lb_kv_cache* cache, const lb_kv_batch* ba
     need(bytes != nullptr, "null host pointer");
     const KvArgs a = kv_args(cache, batch, q_heads);
     check_heads(a);
-    *bytes = a.n_seqs ? attend_plan(a, cache->head_dim, LB_F32).part_floats * 4 : 0;
+    *bytes = a.n_seqs ? checked_plan(a, cache->head_dim, LB_F32).part_floats * 4 : 0;
     return hipSuccess;
   });
 }
@@ -226,9 +233,7 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     check_rows(q, q_stride, width, dtype, rows, "null device pointer: q", "q must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     check_rows(out, out_stride, width, dtype, rows, "null device pointer: out", "out must be 16-B aligned, its row stride at least q_heads * head_dim and a multiple of 16 B");
     if (rows == 0) return hipSuccess;
-    const AttendPlan p = attend_plan(A.kv, cache->head_dim, dtype);
-    need(static_cast<int64_t>(A.kv.n_seqs) * p.tiles * A.kv.kv_heads * p.splits <= kMostGroups && p.units * A.kv.kv_heads <= kMostGroups,
-         "too much work for one call: n_seqs or n_rows * q_heads is too large");
+    const AttendPlan p = checked_plan(A.kv, cache->head_dim, dtype);
     need(p.part_floats == 0 || (workspace && aligned(workspace) && workspace_bytes >= p.part_floats * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_kv_attend_workspace says");
     A.q = q;
@@ -240,6 +245,8 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
     A.scale2 = scale * kLog2e;
     A.window = window < (1 << 30) ? window : 0;  // a sequence has at most 2^30 tokens
     A.tiles = p.tiles;
+    A.few_units = static_cast<uint32_t>(p.few_units);
+    A.jobs = static_cast<uint32_t>(p.jobs);
     A.splits = p.splits;
     A.part_rows = p.part_rows;
     A.units = p.units;

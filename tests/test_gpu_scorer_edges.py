@@ -8,7 +8,7 @@ import torch
 import paper_2603_14002_amd as lbm
 from tests import scorer_ref as ref
 from tests.gpu_util import say
-from tests.test_gpu_scorer import DT, close, dev, handles, randn
+from tests.test_gpu_scorer import DT, bounds, close, dev, handles, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +57,122 @@ def test_attend_bf16_rounds_the_output_alone(case):
             rest = (2.0 ** -16 + 4 * delta + length[s] * 2.0 ** -24).unsqueeze(-1) * mass
             close(out[m:m + n], want, ref.EPS[torch.bfloat16] * (want.abs() + rest) + rest, f"sequence {s}")
         m += n
+
+
+# ------------------------------------------------------------------ batches whose max_new is a loose bound
+
+
+def filled(R, rng, shared=False):
+    """R with keys and values for all tokens (shared: the same ones for every sequence)."""
+    most = max(R.length)
+    k, v = (randn(rng, most, R.H, R.D, dtype=torch.float64) for _ in range(2))
+    for s, n in enumerate(R.length):
+        if not shared:
+            k, v = (randn(rng, n, R.H, R.D, dtype=torch.float64) for _ in range(2))
+        R.put(s, k[:n], v[:n])
+    return R
+
+
+def check_some(R, q, out, lse, scale, window, which):
+    at = np.cumsum([0] + R.new)
+    for s in which:
+        m, n = int(at[s]), R.new[s]
+        if n == 0:
+            continue
+        k, v = R.get(s, R.length[s])
+        want, wl, mass, reach = ref.attend(q.cpu()[m:m + n].double(), k, v, scale, R.length[s] - n, window)
+        b, bl = bounds(want, wl, mass, reach, q.dtype, R.D, R.length[s])
+        close(out[m:m + n], want, b, f"sequence {s}")
+        close(lse[m:m + n], wl, bl, f"lse of sequence {s}")
+
+
+def batch_of(R, max_new):
+    word = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    cache = lbm.KVCache(dev(R.pages), R.P, R.H, R.D, flags=word)
+    return cache, lbm.KVBatch(dev(R.starts), dev(R.lengths), dev(R.table), R.n_rows, max_new)
+
+
+@pytest.mark.parametrize("seqs,heads,max_new,window", [(8192, 8, 8192, 0), (600, 3, 300, 5), (70, 2, 1 << 20, 0), (3, 1, 3, 0)])
+def test_attend_single_tokens_under_a_loose_bound(seqs, heads, max_new, window):
+    """max_new is a bound: a large one gives what the exact one gives, bit for bit where no key range has parts."""
+    say(f"[case] loose {seqs} {heads} {max_new}")
+    rng = np.random.default_rng(40)
+    R = filled(ref.Ragged([1] * seqs, [1 + i % 23 for i in range(seqs)], 16, heads, 64, seed=41), rng, shared=True)
+    q = dev(randn(rng, seqs, heads, 64, dtype=torch.bfloat16))
+    exact = lbm.lb_kv_attend(*batch_of(R, 1), q, 0.3, window=window, want_lse=True)
+    cache, batch = batch_of(R, max_new)
+    loose = lbm.lb_kv_attend(cache, batch, q, 0.3, window=window, want_lse=True)
+    assert cache.status() == 0
+    for a, b in zip(exact, loose):
+        assert torch.equal(a, b)
+    check_some(R, q, *loose, 0.3, window, range(0, seqs, max(1, seqs // 40)))
+
+
+@pytest.mark.parametrize("new,length,P,Hq,H,D,window,t", [
+    ([1] * 40 + [200, 0, 3], [5 + i for i in range(40)] + [260, 9, 70], 16, 8, 2, 64, 0, "bf16"),
+    ([200] + [1] * 7, [300] + [3000 + i for i in range(7)], 64, 2, 2, 128, 0, "f32"),          # parts of the keys
+    ([90, 0, 0, 1, 1, 1, 17, 1], [90, 0, 40, 1100, 2, 1, 17, 1200], 32, 4, 1, 256, 50, "f16"),  # parts, empty sequences
+    ([1] * 1500 + [33], [1 + i % 30 for i in range(1500)] + [500], 16, 16, 4, 64, 0, "bf16"),   # jobs by wavefront
+    ([0] * 20 + [100] + [0] * 20, [3] * 20 + [120] + [7] * 20, 16, 1, 1, 128, 0, "bf16"),
+])
+def test_attend_short_sequences_beside_a_long_one(new, length, P, Hq, H, D, window, t):
+    say(f"[case] mixed {len(new)} {Hq} {H} {D}")
+    rng = np.random.default_rng(42)
+    R = filled(ref.Ragged(new, length, P, H, D, seed=43, pad_rows=2), rng, shared=len(new) > 100)
+    q = dev(randn(rng, R.n_rows, Hq, D, dtype=DT[t]))
+    cache, batch = batch_of(R, max(new))
+    out = torch.full((R.n_rows, Hq, D), 7.0, dtype=DT[t], device="cuda:0")
+    lse = torch.full((R.n_rows, Hq), 7.0, device="cuda:0")
+    lbm.lb_kv_attend(cache, batch, q, D ** -0.5, window=window, out=out, lse=lse)
+    assert cache.status() == 0
+    assert bool((out[sum(new):] == 7.0).all()) and bool((lse[sum(new):] == 7.0).all())
+    which = list(range(len(new))) if len(new) < 100 else list(range(0, len(new), 37)) + [len(new) - 1]
+    check_some(R, q, out, lse, D ** -0.5, window, which)
+
+
+def test_attend_mixed_batches_report_starts_and_lengths_that_do_not_fit():
+    """Flagged whichever sequence it is; where the starts are in order, the other sequences get theirs, and no row
+    outside the sequences is written."""
+    rng = np.random.default_rng(44)
+    new, length = [1] * 30 + [40] + [1] * 9, [20] * 30 + [60] + [30] * 9
+    R = filled(ref.Ragged(new, length, 16, 1, 64, seed=45, pad_rows=3), rng)
+    q = dev(randn(rng, R.n_rows, 2, 64))
+    n, S = sum(new), len(new)
+
+    def run(starts=None, lengths=None):
+        T = ref.Ragged(new, length, 16, 1, 64, seed=45, pad_rows=3)
+        T.pages = R.pages
+        if starts is not None:
+            T.starts = torch.tensor(starts, dtype=torch.int32)
+        if lengths is not None:
+            T.lengths = torch.tensor(lengths, dtype=torch.int32)
+        cache, batch = batch_of(T, 40)
+        out, lse = torch.full((R.n_rows, 2, 64), 7.0, device="cuda:0"), torch.full((R.n_rows, 2), 7.0, device="cuda:0")
+        lbm.lb_kv_attend(cache, batch, q, 0.2, out=out, lse=lse)
+        return out, lse, cache.status()
+
+    say("[case] mixed, bad starts and lengths")
+    out, lse, st = run()
+    assert st == 0
+    check_some(R, q, out, lse, 0.2, 0, range(S))
+    good = R.starts.tolist()
+    for s in (0, 7, 30, S - 1):
+        for value in (-1, 10 ** 9):
+            bad = list(length)
+            bad[s] = value
+            o, l, st = run(lengths=bad)
+            rest = [i for i in range(R.n_rows) if not good[s] <= i < good[s + 1]]
+            assert st & lbm.LB_KV_BAD_LENGTH  # beside it LB_KV_BAD_PAGE, where the length reaches the table's end
+            assert torch.equal(o[rest], out[rest]) and torch.equal(l[rest], lse[rest])
+    # the last sequences past the rows
+    o, l, st = run(starts=good[:-1] + [R.n_rows + 5])
+    assert st == lbm.LB_KV_BAD_LENGTH and torch.equal(o[:n - 1], out[:n - 1])
+    # out of order, far outside
+    for s, value in ((1, -5), (20, -2 ** 31), (20, 2 ** 31 - 1), (31, 2), (0, 9), (S, 3)):
+        starts = list(good)
+        starts[s] = value
+        o, l, st = run(starts=starts)
+        assert st & lbm.LB_KV_BAD_LENGTH
+        assert bool(torch.isfinite(o).all())
+    zero = run(starts=[0] * (S + 1))
+    assert zero[2] == 0 and bool((zero[0] == 7.0).all()) and bool((zero[1] == 7.0).all())

@@ -264,3 +264,22 @@ def test_reference_attention_by_hand():
     out, lse, _, _ = ref.attend(q, k, v, 1.0, 1, 0)
     assert abs(float(out[0, 0, 1]) - 7.0) < 1e-12 and abs(float(lse[0, 0]) - math.log(4)) < 1e-12
     assert abs(float(ref.attend(q, k, v, 1.0, 1, 1)[0][0, 0, 1]) - 8.0) < 1e-12
+
+
+def test_attend_workspace_refuses_what_attend_refuses():
+    """Batches of more work than a call takes, and those that the header says are taken."""
+    n = ctypes.c_int64()
+
+    def workspace(**over):
+        c, b = cache(kv_heads=over.pop("kv_heads")), batch(**over)
+        return lbm.lib().lb_kv_attend_workspace(by(c), by(b), c.kv_heads, ctypes.addressof(n))
+
+    big = dict(kv_heads=1024, n_seqs=1 << 20, n_rows=1 << 20)
+    b = dict(big)
+    assert refused(attend(c=cache(kv_heads=b.pop("kv_heads")), hq=1024, qs=65536, os_=65536, b=batch(**b)))
+    assert refused(workspace(**big))
+    # kv_heads * (n_seqs + n_rows / 16) below 2^24, with any max_new
+    for heads, seqs, rows, new in ((8, 8192, 8192, 8192), (3, 20000, 25000, 5000), (1, 60000, 70000, 10000), (1, 1 << 22, 1 << 24, 1 << 24),
+                                   (15, 1 << 20, 1 << 20, 1), (15, 1 << 20, 1 << 20, 1 << 20)):
+        assert heads * (seqs + rows / 16) < 1 << 24
+        assert workspace(kv_heads=heads, n_seqs=seqs, n_rows=rows, max_new=new) == lbm.LB_OK
