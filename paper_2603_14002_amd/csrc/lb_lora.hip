@@ -332,9 +332,24 @@ hipError_t run(const LoraArgs& A, hipStream_t st) {
   return hipGetLastError();
 }
 
+// A launch has fewer than 2^32 threads: more rows are taken a part at a time.
 template <typename T>
 hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
-  return A.rank <= 16 ? run<T, 1>(A, st) : A.rank <= 32 ? run<T, 2>(A, st) : A.rank <= 64 ? run<T, 4>(A, st) : run<T, 8>(A, st);
+  const int64_t chunks = (A.d_out + int64_t{kUpChannels} - 1) / kUpChannels, up = ((1 << 24) - 1) / chunks;
+  constexpr int64_t down = (int64_t{1} << 32) / (64 * kDownWaves) - 1;
+  const int64_t most = 16 * (up < down ? up : down);
+  for (int64_t row0 = 0; row0 < A.rows; row0 += most) {
+    LoraArgs B = A;
+    B.rows = static_cast<int32_t>(A.rows - row0 < most ? A.rows - row0 : most);
+    B.x = static_cast<const T*>(A.x) + row0 * A.x_stride;
+    B.y = static_cast<const T*>(A.y) + row0 * A.y_stride;
+    B.out = static_cast<T*>(A.out) + row0 * A.out_stride;
+    B.adapter = A.adapter + row0;
+    if (A.h) B.h = A.h + row0 * A.rank;
+    const hipError_t e = A.rank <= 16 ? run<T, 1>(B, st) : A.rank <= 32 ? run<T, 2>(B, st) : A.rank <= 64 ? run<T, 4>(B, st) : run<T, 8>(B, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace

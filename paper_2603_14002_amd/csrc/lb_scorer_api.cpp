@@ -286,7 +286,6 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     need(aligned(a) && aligned(b), "a and b must be 16-B aligned");
     need(adapter || rows == 0, "null device pointer: adapter");
     if (rows == 0) return hipSuccess;
-    need(((rows + 15) / 16) * ((d_out + 255) / 256) <= kMostGroups, "too much work for one call: rows * d_out is too large");
     LoraArgs A{};
     need(lora_whole(rows, d_in, d_out, rank) || (workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4),
          "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says");

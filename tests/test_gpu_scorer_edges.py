@@ -176,3 +176,31 @@ def test_attend_mixed_batches_report_starts_and_lengths_that_do_not_fit():
         assert bool(torch.isfinite(o).all())
     zero = run(starts=[0] * (S + 1))
     assert zero[2] == 0 and bool((zero[0] == 7.0).all()) and bool((zero[1] == 7.0).all())
+
+
+# ------------------------------------------------------------------ adapters
+
+
+def test_lora_rows_past_one_launch():
+    """2^27 rows and more are several launches: the rows are those of a call on each half."""
+    half = 2 ** 26 + 16
+    rows = 2 * half
+    say("[case] lora 2^27 rows")
+    g = torch.Generator(device="cuda:0").manual_seed(50)
+    x, y = (torch.randn(rows, 8, generator=g, device="cuda:0", dtype=torch.bfloat16) for _ in range(2))
+    a, b = (torch.randn(3, 8, 8, generator=g, device="cuda:0", dtype=torch.bfloat16) for _ in range(2))
+    adapter = torch.randint(-1, 3, (rows,), generator=g, device="cuda:0", dtype=torch.int32)
+    out = torch.empty_like(y)
+    lbm.lb_lora_add(y, x, a, b, adapter, out=out)
+    for at in (0, 16 * (2 ** 23 - 1) - 8, rows - 30):
+        rest = slice(at, at + 30)
+        ids = adapter[rest].long()
+        h = torch.bmm(a.float()[ids.clamp_min(0)], x[rest].float().unsqueeze(2))
+        add = torch.bmm(b.float()[ids.clamp_min(0)], h).squeeze(2)
+        want = y[rest].float() + torch.where(ids[:, None] >= 0, add, 0.0)
+        # the output's half step; sums of 8 terms in 32 bits and h in two pieces (2^-16) within |b| |a| |x|
+        size = torch.bmm(b.float().abs()[ids.clamp_min(0)], torch.bmm(a.float().abs()[ids.clamp_min(0)], x[rest].float().abs().unsqueeze(2))).squeeze(2)
+        close(out[rest], want.cpu().double(), (ref.EPS[torch.bfloat16] * want.abs() + 2.0 ** -14 * size).cpu().double(), f"rows {at}")
+    for part in (slice(0, half), slice(half, rows)):
+        lbm.lb_lora_add(y[part], x[part], a, b, adapter[part])  # in place
+    assert torch.equal(out, y)
