@@ -178,7 +178,7 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
  *   adapter device int32 [rows];  scale: device float32 [n_adapters], NULL: 1
  *   workspace  device, 16-B aligned, at least what lb_lora_workspace says for
  *              these rows and sizes (NULL if that is 0)
- * rows at most 2^28.
+ * rows at most 2^28, d_in and d_out 2^30.
  * rank, d_in, d_out are multiples of 8, rank at most 128 (adapters of lower rank
  * are padded with zeros); strides are multiples of 16 B, pointers 16-B aligned. */
 lb_status lb_lora_workspace(int64_t rows, int32_t d_in, int32_t d_out, int32_t rank, int64_t* bytes);

@@ -69,6 +69,12 @@ void check_rows(const void* p, int64_t stride, int64_t width, int32_t dtype, int
   need(aligned(p) && stride >= width && (stride * size_of(dtype)) % 16 == 0 && stride <= (int64_t{1} << 40), layout);
 }
 
+// kernels step past the last channel by up to 2048, in 32 bits
+void check_widths(int32_t d_in, int32_t d_out) {
+  need(d_in >= 8 && d_in % 8 == 0 && d_out >= 8 && d_out % 8 == 0 && d_in <= (1 << 30) && d_out <= (1 << 30),
+       "d_in and d_out must be positive multiples of 8, at most 2^30");
+}
+
 KvArgs kv_args(const lb_kv_cache* c, const lb_kv_batch* b, int32_t q_heads) {
   need(c && b, "null descriptor");
   need(c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256, "head_dim must be 64, 128 or 256");
@@ -262,7 +268,7 @@ lb_status lb_lora_workspace(int64_t rows, int32_t d_in, int32_t d_out, int32_t r
     need(bytes != nullptr, "null host pointer");
     need(rows >= 0 && rows <= (1 << 28), "rows must be in 0..2^28");
     need(rank >= 8 && rank <= 128 && rank % 8 == 0, "rank must be a multiple of 8, at most 128");
-    need(d_in >= 8 && d_in % 8 == 0 && d_out >= 8 && d_out % 8 == 0, "d_in and d_out must be positive multiples of 8");
+    check_widths(d_in, d_out);
     *bytes = lora_whole(rows, d_in, d_out, rank) ? 0 : rows * rank * 4;
     return hipSuccess;
   });
@@ -276,7 +282,7 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     check_dtype(dtype);
     need(rows >= 0 && rows <= (1 << 28), "rows must be in 0..2^28");
     need(rank >= 8 && rank <= 128 && rank % 8 == 0, "rank must be a multiple of 8, at most 128");
-    need(d_in >= 8 && d_in % 8 == 0 && d_out >= 8 && d_out % 8 == 0, "d_in and d_out must be positive multiples of 8");
+    check_widths(d_in, d_out);
     need(n_adapters >= 0, "n_adapters must not be negative");
     check_rows(x, x_stride, d_in, dtype, rows, "null device pointer: x", "x must be 16-B aligned, its row stride at least d_in and a multiple of 16 B");
     check_rows(y, y_stride, d_out, dtype, rows, "null device pointer: y", "y must be 16-B aligned, its row stride at least d_out and a multiple of 16 B");

@@ -283,3 +283,12 @@ def test_attend_workspace_refuses_what_attend_refuses():
                                    (15, 1 << 20, 1 << 20, 1), (15, 1 << 20, 1 << 20, 1 << 20)):
         assert heads * (seqs + rows / 16) < 1 << 24
         assert workspace(kv_heads=heads, n_seqs=seqs, n_rows=rows, max_new=new) == lbm.LB_OK
+
+
+@pytest.mark.parametrize("d_in,d_out", [((1 << 30) + 8, 64), (64, (1 << 30) + 8), (2 ** 31 - 8, 64), (64, 2 ** 31 - 8)])
+def test_lora_widths_past_what_kernels_count(d_in, d_out):
+    a = [1, 1, d_in, d_out, 8, 2, AT, d_in, AT, d_out, AT, AT, AT, None, 2 * AT, d_out, AT, 1 << 20, None]
+    assert refused(lbm.lib().lb_lora_add(*a))
+    n = ctypes.c_int64()
+    assert refused(lbm.lib().lb_lora_workspace(1, d_in, d_out, 8, ctypes.addressof(n)))
+    assert lbm.lib().lb_lora_workspace(1, 1 << 30, 1 << 30, 8, ctypes.addressof(n)) == lbm.LB_OK
