@@ -173,7 +173,8 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
  * lie together (where they do, its weights are read once for all of them).
  * Products are summed in 32 bits and the sum is rounded once.
  *   x       device [rows][d_in], y, out device [rows][d_out], of `dtype`, with
- *           row strides; out may be y itself with the same stride
+ *           row strides; out may be y itself with the same stride, and may
+ *           overlap x, where the workspace has 4 * rows * rank bytes at least
  *   a, b    device [n_adapters][rank][d_in] and [n_adapters][d_out][rank]
  *   adapter device int32 [rows];  scale: device float32 [n_adapters], NULL: 1
  *   workspace  device, 16-B aligned, at least what lb_lora_workspace says for

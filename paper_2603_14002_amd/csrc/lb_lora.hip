@@ -310,34 +310,31 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
 }
 
 template <typename T, int RT>
-hipError_t run(const LoraArgs& A, hipStream_t st) {
+hipError_t down(const LoraArgs& A, hipStream_t st) {
   const unsigned tiles = static_cast<unsigned>((A.rows + 15) / 16);
-  const unsigned chunks = static_cast<unsigned>((A.d_out + kUpChannels - 1) / kUpChannels);
   // few tiles: the adapters of a tile side by side
-  const unsigned down = tiles < 512 ? 16 : 1, up = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
-  if constexpr (RT <= 2)
-    if (lora_whole(A.rows, A.d_in, A.d_out, A.rank)) {
-      k_lora_up<T, RT, true><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
-      return hipGetLastError();
-    }
+  const unsigned turns = tiles < 512 ? 16 : 1;
   // and with very few the rank's tiles too, each with its part of A, but x read again for each (rank 64, d_in 2048,
   // bf16, d_out 512: 16 rows 9.6 us, else 15.3; 512 rows of their own adapters 34.7, else 30.4)
   if (RT > 1 && tiles < 16)
-    k_lora_down<T, 1><<<dim3(tiles, down, (A.rank + 15) / 16), 64 * kDownWaves, 0, st>>>(A);
+    k_lora_down<T, 1><<<dim3(tiles, turns, (A.rank + 15) / 16), 64 * kDownWaves, 0, st>>>(A);
   else
-    k_lora_down<T, RT><<<dim3(tiles, down), 64 * kDownWaves, 0, st>>>(A);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  k_lora_up<T, RT, false><<<dim3(tiles * chunks, up), 256, 0, st>>>(A);
+    k_lora_down<T, RT><<<dim3(tiles, turns), 64 * kDownWaves, 0, st>>>(A);
   return hipGetLastError();
 }
 
-// A launch has fewer than 2^32 threads: more rows are taken a part at a time.
-template <typename T>
-hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
-  const int64_t chunks = (A.d_out + int64_t{kUpChannels} - 1) / kUpChannels, up = ((1 << 24) - 1) / chunks;
-  constexpr int64_t down = (int64_t{1} << 32) / (64 * kDownWaves) - 1;
-  const int64_t most = 16 * (up < down ? up : down);
+template <typename T, int RT, bool whole>
+hipError_t up(const LoraArgs& A, hipStream_t st) {
+  const unsigned tiles = static_cast<unsigned>((A.rows + 15) / 16);
+  const unsigned chunks = static_cast<unsigned>((A.d_out + kUpChannels - 1) / kUpChannels);
+  const unsigned turns = static_cast<int64_t>(tiles) * chunks < 512 ? 16 : 1;
+  k_lora_up<T, RT, whole><<<dim3(tiles * chunks, turns), 256, 0, st>>>(A);
+  return hipGetLastError();
+}
+
+// f of `most` rows at a time
+template <typename T, typename F>
+hipError_t each_part(const LoraArgs& A, int64_t most, F&& f) {
   for (int64_t row0 = 0; row0 < A.rows; row0 += most) {
     LoraArgs B = A;
     B.rows = static_cast<int32_t>(A.rows - row0 < most ? A.rows - row0 : most);
@@ -345,11 +342,29 @@ hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
     B.y = static_cast<const T*>(A.y) + row0 * A.y_stride;
     B.out = static_cast<T*>(A.out) + row0 * A.out_stride;
     B.adapter = A.adapter + row0;
-    if (A.h) B.h = A.h + row0 * A.rank;
-    const hipError_t e = A.rank <= 16 ? run<T, 1>(B, st) : A.rank <= 32 ? run<T, 2>(B, st) : A.rank <= 64 ? run<T, 4>(B, st) : run<T, 8>(B, st);
+    B.h = A.h + row0 * A.rank;
+    const hipError_t e = f(B);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+// A launch has fewer than 2^32 threads: more rows are taken a part at a time, all of x
+// read before the first of out is written, which may overlap it.
+template <typename T, int RT>
+hipError_t run(const LoraArgs& A, hipStream_t st) {
+  if constexpr (RT <= 2)
+    if (A.whole) return up<T, RT, true>(A, st);
+  const int64_t chunks = (A.d_out + kUpChannels - 1) / kUpChannels;
+  constexpr int64_t threads = (int64_t{1} << 32) - 1;
+  const hipError_t e = each_part<T>(A, 16 * (threads / (64 * kDownWaves)), [&](const LoraArgs& B) { return down<T, RT>(B, st); });
+  if (e != hipSuccess) return e;
+  return each_part<T>(A, 16 * (threads / (256 * chunks)), [&](const LoraArgs& B) { return up<T, RT, false>(B, st); });
+}
+
+template <typename T>
+hipError_t by_rank(const LoraArgs& A, hipStream_t st) {
+  return A.rank <= 16 ? run<T, 1>(A, st) : A.rank <= 32 ? run<T, 2>(A, st) : A.rank <= 64 ? run<T, 4>(A, st) : run<T, 8>(A, st);
 }
 
 }  // namespace

@@ -62,6 +62,7 @@ struct LoraArgs {
   float* h;
   int64_t x_stride, y_stride, out_stride;
   int32_t rows, d_in, d_out, rank, n_adapters;
+  bool whole;  // in one launch
 };
 
 struct LogitArgs {
@@ -96,7 +97,7 @@ hipError_t launch_kv_append(const AppendArgs& A, int head_dim, int dtype, hipStr
 hipError_t launch_kv_read(const ReadArgs& A, int head_dim, int dtype, hipStream_t st);
 hipError_t launch_kv_attend(const AttendArgs& A, int head_dim, int dtype, hipStream_t st);
 
-// the call is one launch, and needs no workspace
+// the call is one launch, and needs no workspace (if out and x have no memory in common)
 bool lora_whole(int64_t rows, int32_t d_in, int32_t d_out, int32_t rank);
 hipError_t launch_lora(const LoraArgs& A, int dtype, hipStream_t st);
 

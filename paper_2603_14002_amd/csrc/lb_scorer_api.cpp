@@ -75,6 +75,18 @@ void check_widths(int32_t d_in, int32_t d_out) {
        "d_in and d_out must be positive multiples of 8, at most 2^30");
 }
 
+// whether two matrices of rows have memory in common (true where strides differ and
+// their ranges meet)
+bool overlap(const void* a, int64_t a_stride, int64_t a_width, const void* b, int64_t b_stride, int64_t b_width, int64_t rows, int64_t size) {
+  const __int128 at = reinterpret_cast<uintptr_t>(a), bt = reinterpret_cast<uintptr_t>(b);
+  const __int128 a_end = at + (static_cast<__int128>(rows - 1) * a_stride + a_width) * size;
+  const __int128 b_end = bt + (static_cast<__int128>(rows - 1) * b_stride + b_width) * size;
+  if (a_end <= bt || b_end <= at) return false;
+  if (a_stride != b_stride) return true;
+  const int64_t line = a_stride * size, from = static_cast<int64_t>(((bt - at) % line + line) % line);  // of b in a's rows
+  return from < a_width * size || from + b_width * size > line;
+}
+
 KvArgs kv_args(const lb_kv_cache* c, const lb_kv_batch* b, int32_t q_heads) {
   need(c && b, "null descriptor");
   need(c->head_dim == 64 || c->head_dim == 128 || c->head_dim == 256, "head_dim must be 64, 128 or 256");
@@ -293,8 +305,10 @@ lb_status lb_lora_add(int32_t dtype, int64_t rows, int32_t d_in, int32_t d_out, 
     need(adapter || rows == 0, "null device pointer: adapter");
     if (rows == 0) return hipSuccess;
     LoraArgs A{};
-    need(lora_whole(rows, d_in, d_out, rank) || (workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4),
-         "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says");
+    // one launch reads x while other workgroups write out
+    A.whole = lora_whole(rows, d_in, d_out, rank) && !overlap(x, x_stride, d_in, out, out_stride, d_out, rows, size_of(dtype));
+    need(A.whole || (workspace && aligned(workspace) && workspace_bytes >= rows * rank * 4),
+         "the workspace is null, not 16-B aligned or smaller than lb_lora_workspace says (4 * rows * rank bytes where out and x overlap)");
     A.x = x;
     A.y = y;
     A.a = a;

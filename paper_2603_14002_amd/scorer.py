@@ -447,9 +447,13 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     if x.get_device() != g or a.get_device() != g or b.get_device() != g or adapter.get_device() != g or out.get_device() != g \
             or (scale is not None and scale.get_device() != g):
         _elsewhere(g, x=x, a=a, b=b, adapter=adapter, scale=scale, out=out)
-    ws, nbytes, _held = _scratch(y, stream, 0 if workspace is not None else lb_lora_workspace(rows, d_in, d_out, rank), workspace, "lb_lora_add")
-    _call(g, stream, "lb_lora_add", dt, rows, d_in, d_out, rank, n, x.data_ptr(), xs, y.data_ptr(), ys, a.data_ptr(),
-          b.data_ptr(), adapter.data_ptr(), _ptr(scale), out.data_ptr(), os, ws, nbytes)
+    xp, op = x.data_ptr(), out.data_ptr()
+    need = 0 if workspace is not None else lb_lora_workspace(rows, d_in, d_out, rank)
+    if need == 0 and -4 * rows * os < op - xp < 4 * rows * xs:  # at most 4 B a value: they may overlap
+        need = 4 * rows * rank
+    ws, nbytes, _held = _scratch(y, stream, need, workspace, "lb_lora_add")
+    _call(g, stream, "lb_lora_add", dt, rows, d_in, d_out, rank, n, xp, xs, y.data_ptr(), ys, a.data_ptr(),
+          b.data_ptr(), adapter.data_ptr(), _ptr(scale), op, os, ws, nbytes)
     return out
 
 

@@ -204,3 +204,32 @@ def test_lora_rows_past_one_launch():
     for part in (slice(0, half), slice(half, rows)):
         lbm.lb_lora_add(y[part], x[part], a, b, adapter[part])  # in place
     assert torch.equal(out, y)
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,d,r", [(8, 512, 16), (40, 1024, 8), (256, 264, 8), (20, 512, 64), (600, 272, 16)])
+def test_lora_over_its_own_input(rows, d, r, t):
+    """x is y, or lies across the result: as if x had been copied first, in one launch's sizes and in two's."""
+    say(f"[case] lora over x {rows} {d} {r} {t}")
+    rng = np.random.default_rng(51)
+    dt = DT[t]
+    wide = dev(randn(rng, rows, 2 * d, dtype=dt))
+    a, b = dev(randn(rng, 5, r, d, dtype=dt) * 0.1), dev(randn(rng, 5, d, r, dtype=dt) * 0.1)
+    adapter = dev(torch.from_numpy(rng.integers(-1, 5, rows).astype(np.int32)))
+    for off in (0, 8, d - 8, d):  # out lies `off` channels into x: the same, overlapping, beside it
+        apart = lbm.lb_lora_add(wide[:, off:off + d].clone(), wide[:, :d].clone(), a, b, adapter)
+        for _ in range(8):
+            one = wide.clone()
+            lbm.lb_lora_add(one[:, off:off + d], one[:, :d], a, b, adapter)
+            # one launch sums h's parts of 4 wavefronts, two of 8: the same up to 32-bit sums' order
+            bound = 2.0 ** -20 * apart.abs().amax() + 2 * ref.EPS[dt] * apart.abs()
+            close(one[:, off:off + d], apart.cpu().double(), bound.cpu().double(), f"offset {off}")
+            assert torch.equal(one[:, off + d:], wide[:, off + d:]) and torch.equal(one[:, :off], wide[:, :off])
+    # rows over other rows
+    tall = dev(randn(rng, rows + 16, d, dtype=dt))
+    for x0, y0 in ((0, 16), (16, 0)):
+        apart = lbm.lb_lora_add(tall[y0:y0 + rows].clone(), tall[x0:x0 + rows].clone(), a, b, adapter)
+        one = tall.clone()
+        lbm.lb_lora_add(one[y0:y0 + rows], one[x0:x0 + rows], a, b, adapter)
+        bound = 2.0 ** -20 * apart.abs().amax() + 2 * ref.EPS[dt] * apart.abs()
+        close(one[y0:y0 + rows], apart.cpu().double(), bound.cpu().double(), f"rows {x0} {y0}")

@@ -292,3 +292,14 @@ def test_lora_widths_past_what_kernels_count(d_in, d_out):
     n = ctypes.c_int64()
     assert refused(lbm.lib().lb_lora_workspace(1, d_in, d_out, 8, ctypes.addressof(n)))
     assert lbm.lib().lb_lora_workspace(1, 1 << 30, 1 << 30, 8, ctypes.addressof(n)) == lbm.LB_OK
+
+
+def test_lora_over_its_own_input_needs_a_workspace():
+    """A call of one launch would write rows of x that its other workgroups still read."""
+    L = lbm.lib()
+    n = ctypes.c_int64()
+    assert L.lb_lora_workspace(4, 512, 512, 16, ctypes.addressof(n)) == lbm.LB_OK and n.value == 0
+    for x, xs, out, os_ in ((AT, 512, AT, 512), (AT, 512, AT + 64, 512), (AT + 512 * 4 * 3, 512, AT, 512), (AT, 2048, AT + 511 * 4 + 4 - 16, 2048),
+                            (AT + 1600 * 4, 2048, AT, 2048), (AT, 1024, AT + 600 * 4, 1032)):
+        for nb in (0, 4 * 16 * 4 - 1):
+            assert refused(L.lb_lora_add(0, 4, 512, 512, 16, 2, x, xs, out, os_, AT, AT, AT, None, out, os_, AT if nb else None, nb, None))
