@@ -230,7 +230,7 @@ enum { LB_MAX_RULE_IDS = 4096 };
  *             most 2^28, classes 2^30
  *   workspace  device, 16-B aligned, at least what lb_logits_workspace says for
  *              these rows and classes (NULL if that is 0)
- * logits is only read; logprobs may be the logits themselves where these are
+ * A call made again gives the same bits.  logits is only read; logprobs may be the logits themselves where these are
  * LB_F32 with the same stride. */
 lb_status lb_logits_workspace(int64_t rows, int32_t classes, int64_t* bytes);
 lb_status lb_logits_adjust(int32_t dtype, int64_t rows, int32_t classes, const void* logits,

@@ -142,9 +142,10 @@ constexpr int kPartClasses = 131072;  // classes of one part at most: 16 KB of b
 struct Slot {
   int32_t id;     // -1: empty
   int32_t count;  // occurrences in the history
-  int32_t bias;   // place in the bias list + 1, 0: none
+  int32_t entry;  // the entry that answers for the class: its last bias (kBias + place), else its first occurrence (history_width - place)
   float x;        // the class's logit after the rules up to the temperature
 };
+constexpr int32_t kBias = LB_MAX_RULE_IDS + 1;
 
 // A part of a row: the classes lo .. hi - 1, in chunks of eight that start at
 // 16-B aligned logits (the first and last may be cut short).  bit 8 c + i of
@@ -160,6 +161,8 @@ struct Part {
   int32_t slots;
   bool sparse;  // some bit may be clear (other than outside the part)
   float k;
+  const int32_t *past, *biased;  // the row's lists
+  int32_t H, W;
 
   __device__ __forceinline__ void start(const LogitArgs& A, int64_t row, int32_t part, int32_t parts, int32_t n_slots, uint32_t* shared) {
     const int32_t per = (A.classes + parts - 1) / parts;
@@ -193,9 +196,11 @@ struct Part {
     }
     for (int32_t i = threadIdx.x; i < slots; i += 256) table[i] = Slot{-1, 0, 0, 0.0f};
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < A.r.history_width; i += 256) put(A.r.history[row * A.r.history_width + i], 1, 0);
-    const int64_t list = A.r.bias_per_row ? row * A.r.bias_width : 0;
-    for (int32_t i = threadIdx.x; i < A.r.bias_width; i += 256) put(A.r.bias_ids[list + i], 0, i + 1);
+    H = A.r.history_width, W = A.r.bias_width;
+    const int64_t list = A.r.bias_per_row ? row * W : 0;
+    past = A.r.history + row * H, biased = A.r.bias_ids + list;
+    for (int32_t i = threadIdx.x; i < H; i += 256) put(past[i], 1, H - i);
+    for (int32_t i = threadIdx.x; i < W; i += 256) put(biased[i], 0, kBias + i);
     __syncthreads();
     for (int32_t i = threadIdx.x; i < slots; i += 256) {
       Slot& s = table[i];
@@ -203,7 +208,7 @@ struct Part {
       const int32_t at = s.id - first;
       if (shared[at >> 5] >> (at & 31) & 1u) {
         atomicAnd(&shared[at >> 5], ~(1u << (at & 31)));
-        s.x = rules(as_float(src[s.id]), s.count, s.bias ? A.r.bias_values[list + s.bias - 1] : 0.0f);
+        s.x = rules(as_float(src[s.id]), s.count, s.entry >= kBias ? A.r.bias_values[list + s.entry - kBias] : 0.0f);
       } else {
         s.x = -__builtin_inff();  // masked
       }
@@ -211,16 +216,24 @@ struct Part {
     __syncthreads();
   }
 
-  __device__ __forceinline__ void put(int32_t id, int32_t count, int32_t bias) {
-    if (id < lo || id >= hi) return;
-    uint32_t at = (static_cast<uint32_t>(id) * 2654435761u) & (slots - 1);
+  __device__ __forceinline__ bool inside(int32_t id) const { return id >= lo && id < hi; }
+  __device__ __forceinline__ uint32_t first_slot(int32_t id) const { return (static_cast<uint32_t>(id) * 2654435761u) >> (__builtin_clz(slots) + 1); }
+  __device__ __forceinline__ void put(int32_t id, int32_t count, int32_t entry) {
+    if (!inside(id)) return;
+    uint32_t at = first_slot(id);
     for (;;) {
       const int32_t was = atomicCAS(&table[at].id, -1, id);
       if (was == -1 || was == id) break;
       at = (at + 1) & (slots - 1);
     }
     if (count) atomicAdd(&table[at].count, count);
-    if (bias) atomicMax(&table[at].bias, bias);
+    atomicMax(&table[at].entry, entry);
+  }
+  // the slot of a class, or the empty one where it would be (half of the slots are empty at least)
+  __device__ __forceinline__ uint32_t find(int32_t id) const {
+    uint32_t at = first_slot(id);
+    while (table[at].id != id && table[at].id >= 0) at = (at + 1) & (slots - 1);
+    return at;
   }
 
   // the logits of chunk c, -infinity where its bits are clear; false: the chunk is cut short
@@ -268,18 +281,27 @@ struct Part {
       add(s, x, k);
     }
     for (; c < chunks; c += 256) one(s, c);
-    for (int32_t i = threadIdx.x; i < slots; i += 256) {
-      if (table[i].id < 0) continue;
-      const float x[1] = {table[i].x};
-      add(s, x, k);
-      if (table[i].id == target) *xt = x[0];
+    // the named classes, each by the thread of the entry that answers for it: the order of the sum is the lists',
+    // not that in which the wavefronts came to the table
+    if (slots) {
+      for (int32_t i = threadIdx.x; i < H; i += 256) named(s, past[i], H - i);
+      for (int32_t i = threadIdx.x; i < W; i += 256) named(s, biased[i], kBias + i);
     }
-    // the target, if it is neither masked nor named
-    if (threadIdx.x == 0 && target >= lo && target < hi) {
+    if (threadIdx.x == 0 && inside(target)) {
       const int32_t at = target - first;
-      if (!sparse || open[at >> 3] >> (at & 7) & 1) *xt = as_float(src[target]);
+      if (!sparse || open[at >> 3] >> (at & 7) & 1)
+        *xt = as_float(src[target]);
+      else if (slots && table[find(target)].id == target)
+        *xt = table[find(target)].x;
     }
     return s;
+  }
+  __device__ __forceinline__ void named(Sum& s, int32_t id, int32_t entry) const {
+    if (!inside(id)) return;
+    const Slot& at = table[find(id)];
+    if (at.entry != entry) return;
+    const float x[1] = {at.x};
+    add(s, x, k);
   }
   __device__ __forceinline__ void one(Sum& s, int32_t c) const {
     float x[8];

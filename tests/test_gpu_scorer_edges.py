@@ -233,3 +233,25 @@ def test_lora_over_its_own_input(rows, d, r, t):
         lbm.lb_lora_add(one[y0:y0 + rows], one[x0:x0 + rows], a, b, adapter)
         bound = 2.0 ** -20 * apart.abs().amax() + 2 * ref.EPS[dt] * apart.abs()
         close(one[y0:y0 + rows], apart.cpu().double(), bound.cpu().double(), f"rows {x0} {y0}")
+
+
+# ------------------------------------------------------------------ logits
+
+
+@pytest.mark.parametrize("R,C,H,W,t", [(64, 125002, 300, 200, "bf16"), (1, 125002, 3000, 1000, "f32"), (400, 700, 60, 68, "f32"), (5, 20000, 1, 4095, "f16")])
+def test_logits_of_long_rows_repeat_bit_for_bit(R, C, H, W, t):
+    """The named classes are added in an order that does not depend on which wavefront came first."""
+    say(f"[case] repeat {R} {C}")
+    rng = np.random.default_rng(60)
+    x = dev((3 * randn(rng, R, C)).to(DT[t]))
+    x += 4.0  # most of a row's sum can lie in the named classes
+    rules = lbm.LogitRules(temperature=0.9, repetition=1.1, presence=0.1, frequency=0.1,
+                           history=dev(torch.from_numpy(rng.integers(0, C, (R, H)).astype(np.int32))),
+                           bias_ids=dev(torch.from_numpy(rng.integers(0, C, (R, W)).astype(np.int32))),
+                           bias_values=dev(randn(rng, R, W) + 9))
+    first = None
+    for _ in range(60):
+        logp, _, lse = lbm.lb_logits_adjust(x, rules)
+        if first is None:
+            first = logp, lse
+        assert torch.equal(lse, first[1]) and torch.equal(logp, first[0])
