@@ -200,7 +200,7 @@ class KVCache:
     [n_pages, kv_heads, page_tokens * (head_dim + head_dim / 16)], `flags` None or an int32
     tensor of one element that faults of the data are or-ed into."""
 
-    __slots__ = ("pages", "flags", "page_tokens", "kv_heads", "head_dim", "device", "desc", "ref")
+    __slots__ = ("pages", "flags", "page_tokens", "kv_heads", "head_dim", "device", "sizes", "desc", "ref")
 
     def __init__(self, pages, page_tokens: int, kv_heads: int, head_dim: int, flags=None):
         if torch is None:
@@ -214,7 +214,7 @@ class KVCache:
         if flags is not None and (flags.dtype is not torch.int32 or flags.numel() != 1 or flags.get_device() != self.device):
             _bad("flags must be one int32 on the pages' device")
         self.pages, self.flags = pages, flags
-        self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
+        self.sizes = self.page_tokens, self.kv_heads, self.head_dim = page_tokens, kv_heads, head_dim
         self.desc = lb_kv_cache(pages.data_ptr(), at[0], page_tokens, kv_heads, head_dim, 0, _ptr(flags))
         self.ref = ctypes.addressof(self.desc)
 
@@ -239,7 +239,7 @@ class KVBatch:
     [n_seqs] and pages [n_seqs, max_pages]; `n_rows` rows of activations, at most `max_new`
     new tokens a sequence.  The tensors may be changed between calls."""
 
-    __slots__ = ("starts", "lengths", "pages", "n_rows", "max_pages", "device", "desc", "ref")
+    __slots__ = ("starts", "lengths", "pages", "n_rows", "max_pages", "device", "sizes", "desc", "ref")
 
     def __init__(self, starts, lengths, pages, n_rows: int, max_new: int):
         if torch is None:
@@ -256,6 +256,7 @@ class KVBatch:
         if lengths.get_device() != g or pages.get_device() != g:
             _elsewhere(g, lengths=lengths, pages=pages)
         self.starts, self.lengths, self.pages, self.n_rows, self.max_pages = starts, lengths, pages, n_rows, at[1]
+        self.sizes = (n, n_rows, at[1], max_new)
         self.desc = lb_kv_batch(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), n, n_rows, at[1], max_new)
         self.ref = ctypes.addressof(self.desc)
 
@@ -388,6 +389,9 @@ def lb_kv_attend_workspace(cache: KVCache, batch: KVBatch, q_heads: int) -> int:
     return need.value
 
 
+_attend_bytes = {}  # what the library has said of these sizes
+
+
 def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 0, out=None, lse=None, want_lse: bool = False,
                  workspace=None, stream=None):
     """Attention of the batch's new tokens, q [n_rows, q_heads, head_dim].  Returns (out, lse): out (or a
@@ -408,9 +412,16 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
         _elsewhere(g, lse=lse)
     elif want_lse:
         lse = _empty((n, hq), torch.float32, q, stream)
-    ws, nbytes, _held = None, 0, None
-    if workspace is not None or batch.max_pages * cache.page_tokens >= 1024:  # shorter key ranges have no parts, and need none
-        ws, nbytes, _held = _scratch(q, stream, 0 if workspace is not None else lb_kv_attend_workspace(cache, batch, hq), workspace, "lb_kv_attend")
+    need = 0
+    if workspace is None:
+        sizes = (cache.sizes, batch.sizes, hq)
+        need = _attend_bytes.get(sizes)
+        if need is None:
+            need = lb_kv_attend_workspace(cache, batch, hq)
+            if len(_attend_bytes) >= 4096:
+                _attend_bytes.clear()
+            _attend_bytes[sizes] = need
+    ws, nbytes, _held = _scratch(q, stream, need, workspace, "lb_kv_attend")
     _call(g, stream, "lb_kv_attend", cache.ref, batch.ref, dt, hq, q.data_ptr(), qs, scale, window, out.data_ptr(), os,
           _ptr(lse), ws, nbytes)
     return out, lse

@@ -303,3 +303,24 @@ def test_lora_over_its_own_input_needs_a_workspace():
                             (AT + 1600 * 4, 2048, AT, 2048), (AT, 1024, AT + 600 * 4, 1032)):
         for nb in (0, 4 * 16 * 4 - 1):
             assert refused(L.lb_lora_add(0, 4, 512, 512, 16, 2, x, xs, out, os_, AT, AT, AT, None, out, os_, AT if nb else None, nb, None))
+
+
+def test_attend_takes_the_workspace_that_the_library_says(monkeypatch):
+    """Whatever the table's width: the rule for parts of the keys is the library's alone."""
+    asked, got = [], []
+
+    def workspace(c, b, heads):
+        asked.append((b.max_pages, heads))
+        return 1024 * b.max_pages + heads
+
+    monkeypatch.setattr(scorer, "lb_kv_attend_workspace", workspace)
+    monkeypatch.setattr(scorer, "_call", lambda g, stream, name, *a: got.append(a[-1]))
+    monkeypatch.setattr(scorer, "_attend_bytes", {})
+    c = lbm.KVCache(torch.zeros(3, 2, 16 * 68, dtype=torch.uint8), 16, 2, 64)
+    i32 = dict(dtype=torch.int32)
+    for width, heads in ((4, 2), (1, 4), (70, 2), (4, 4)):
+        for _ in range(2):  # asked once for each size
+            b = lbm.KVBatch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, width, **i32), 2, 1)
+            lbm.lb_kv_attend(c, b, torch.zeros(2, heads, 64), 1.0)
+            assert got.pop() == 1024 * width + heads
+    assert len(asked) == len(set(asked)) == 4
