@@ -4,8 +4,9 @@ the C ABI, over torch tensors.
 The functions check what the C side cannot see of a tensor (its type, shape, device and
 layout), raise ``LBError`` for it as for the library's own refusals, allocate the outputs
 and workspaces that are not given, and enqueue the call on ``stream`` (None: torch's
-current stream of the tensors' device).  Every step runs in the library's HIP kernels, and
-no gradients are recorded.
+current stream of the tensors' device).  Every step runs in the library's HIP kernels.  No
+gradients are recorded: where torch records them, a tensor that requires one is refused,
+and tensors of the caller's that a call writes to count as changed in place.
 
 A call on few rows is mostly this file's work, so what a function has made itself is not
 checked again, and nothing that the common case does not need is called.
@@ -68,21 +69,21 @@ def declare(L) -> None:
         f.argtypes = at[name]
 
 
-# torch, this package, torch's current raw stream of a device and its current device, set by _load() before
-# the first use: the package can be imported without torch, and a call of a few microseconds has no time for
+# torch, this package, torch's current raw stream of a device, its current device, whether it records gradients
+# and what counts a tensor as changed, set by _load() before the first use: the package can be imported without torch, and a call of a few microseconds has no time for
 # an import statement in each helper
-torch = _lbm = _raw_stream = _current_device = None
+torch = _lbm = _raw_stream = _current_device = _recording = _changed = None
 _DTYPE = {}
 
 
 def _load() -> None:
-    global torch, _lbm, _raw_stream, _current_device
+    global torch, _lbm, _raw_stream, _current_device, _recording, _changed
     if torch is not None:
         return
     import torch as t
     import paper_2603_14002_amd as lbm
     _DTYPE.update({t.float32: LB_F32, t.bfloat16: LB_BF16, t.float16: LB_F16})
-    _lbm, _current_device = lbm, t.cuda.current_device
+    _lbm, _current_device, _recording, _changed = lbm, t.cuda.current_device, t.is_grad_enabled, t.autograd.graph.increment_version
     # what torch.cuda.current_stream(i).cuda_stream reads, without making a Stream object (2.8 us)
     _raw_stream = getattr(t._C, "_cuda_getCurrentRawStream", None) or (lambda i: t.cuda.current_stream(i).cuda_stream)
     torch = t
@@ -121,6 +122,13 @@ def _elsewhere(g: int, **tensors) -> None:
     for name, t in tensors.items():
         if t is not None and t.get_device() != g:
             _bad(f"{name} is on {t.device}, the call's other tensors are on {f'cuda:{g}' if g >= 0 else 'cpu'}")
+
+
+def _no_gradient(**tensors) -> None:
+    """Refuses the call for the first of its tensors that requires a gradient."""
+    for name, t in tensors.items():
+        if t is not None and t.requires_grad:
+            _bad(f"{name} requires a gradient, and none is recorded: call under torch.no_grad(), or detach it")
 
 
 def _empty(shape, dtype, like, stream):
@@ -343,7 +351,11 @@ def lb_kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope: Optional[Rope] =
     ks, vs = _heads(k, "k", n, H, D, dtype), _heads(v, "v", n, H, D, dtype)
     if batch.device != g or k.get_device() != g or v.get_device() != g or (rope is not None and rope.device != g):
         _elsewhere(g, starts=batch.starts, k=k, v=v, cos=None if rope is None else rope.cos)
+    if _recording() and (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad)
+                         or (rope is not None and (rope.cos.requires_grad or rope.sin.requires_grad))):
+        _no_gradient(q=q, k=k, v=v, q_out=q_out, cos=None if rope is None else rope.cos, sin=None if rope is None else rope.sin)
     hq = qs = os = 0
+    written = cache.pages if q_out is None else (cache.pages, q_out)
     if q is not None:
         qs, hq = _heads(q, "q", n, None, D, dtype), q.shape[1]
         if q.get_device() != g or (q_out is not None and q_out.get_device() != g):
@@ -356,6 +368,7 @@ def lb_kv_append(cache: KVCache, batch: KVBatch, q, k, v, rope: Optional[Rope] =
         _bad("q_out needs q")
     _call(g, stream, "lb_kv_append", cache.ref, batch.ref, None if rope is None else rope.ref, dt, hq, _ptr(q), qs,
           k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_out), os)
+    _changed(written)
     return q_out
 
 
@@ -369,6 +382,9 @@ def lb_kv_read(cache: KVCache, batch: KVBatch, dtype=None, k_out=None, v_out=Non
     ks = vs = H * D
     if batch.device != g:
         _elsewhere(g, starts=batch.starts)
+    written = [t for t in (k_out, v_out) if t is not None]
+    if written and _recording():
+        _no_gradient(k_out=k_out, v_out=v_out)
     if k_out is None:
         k_out = _empty((n, H, D), dtype, cache.pages, stream)
     else:
@@ -380,6 +396,8 @@ def lb_kv_read(cache: KVCache, batch: KVBatch, dtype=None, k_out=None, v_out=Non
         vs = _heads(v_out, "v_out", n, H, D, dtype)
         _elsewhere(g, v_out=v_out)
     _call(g, stream, "lb_kv_read", cache.ref, batch.ref, _dtype(k_out, "k_out"), k_out.data_ptr(), ks, v_out.data_ptr(), vs)
+    if written:
+        _changed(written)
     return k_out, v_out
 
 
@@ -401,6 +419,9 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
     hq = q.shape[1]
     if batch.device != g or q.get_device() != g:
         _elsewhere(g, starts=batch.starts, q=q)
+    written = () if out is None and lse is None else [t for t in (out, lse) if t is not None]
+    if _recording() and (q.requires_grad or written):
+        _no_gradient(q=q, out=out, lse=lse)
     if out is None:
         out, os = _empty((n, hq, D), dtype, q, stream), hq * D
     else:
@@ -424,6 +445,8 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
     ws, nbytes, _held = _scratch(q, stream, need, workspace, "lb_kv_attend")
     _call(g, stream, "lb_kv_attend", cache.ref, batch.ref, dt, hq, q.data_ptr(), qs, scale, window, out.data_ptr(), os,
           _ptr(lse), ws, nbytes)
+    if written:
+        _changed(written)
     return out, lse
 
 
@@ -458,6 +481,9 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     if x.get_device() != g or a.get_device() != g or b.get_device() != g or adapter.get_device() != g or out.get_device() != g \
             or (scale is not None and scale.get_device() != g):
         _elsewhere(g, x=x, a=a, b=b, adapter=adapter, scale=scale, out=out)
+    if _recording() and (y.requires_grad or x.requires_grad or a.requires_grad or b.requires_grad or out.requires_grad
+                         or (scale is not None and scale.requires_grad)):
+        _no_gradient(y=y, x=x, a=a, b=b, scale=scale, out=out)
     xp, op = x.data_ptr(), out.data_ptr()
     need = 0 if workspace is not None else lb_lora_workspace(rows, d_in, d_out, rank)
     if need == 0 and -4 * rows * os < op - xp < 4 * rows * xs:  # at most 4 B a value: they may overlap
@@ -465,6 +491,7 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     ws, nbytes, _held = _scratch(y, stream, need, workspace, "lb_lora_add")
     _call(g, stream, "lb_lora_add", dt, rows, d_in, d_out, rank, n, xp, xs, y.data_ptr(), ys, a.data_ptr(),
           b.data_ptr(), adapter.data_ptr(), _ptr(scale), op, os, ws, nbytes)
+    _changed(out)
     return out
 
 
@@ -486,6 +513,9 @@ def lb_logits_adjust(logits, rules: Optional[LogitRules] = None, target=None, wa
         _bad("logits must have 2 dimensions")
     rows, classes = logits.shape
     stride = _rows(logits, "logits", rows, classes, logits.dtype)
+    if _recording() and (logits.requires_grad or logprobs is not None or rules is not None):
+        _no_gradient(logits=logits, logprobs=logprobs, bias_values=None if rules is None else rules.bias_values)
+    written = logprobs
     os = classes
     if logprobs is not None:
         os = _rows(logprobs, "logprobs", rows, classes, torch.float32)
@@ -519,4 +549,6 @@ def lb_logits_adjust(logits, rules: Optional[LogitRules] = None, target=None, wa
     ws, nbytes, _held = _scratch(logits, stream, 0 if workspace is not None else lb_logits_workspace(rows, classes), workspace, "lb_logits_adjust")
     _call(g, stream, "lb_logits_adjust", dt, rows, classes, logits.data_ptr(), stride, ref, _ptr(target), _ptr(logprobs), os,
           _ptr(score), _ptr(lse), ws, nbytes)
+    if written is not None:
+        _changed(written)
     return logprobs, score, lse

@@ -324,3 +324,55 @@ def test_attend_takes_the_workspace_that_the_library_says(monkeypatch):
             lbm.lb_kv_attend(c, b, torch.zeros(2, heads, 64), 1.0)
             assert got.pop() == 1024 * width + heads
     assert len(asked) == len(set(asked)) == 4
+
+
+def small():
+    """A call of every function of the binding: its tensors by name, which of them it writes to, and the call."""
+    i32 = dict(dtype=torch.int32)
+    c = lbm.KVCache(torch.zeros(3, 2, 16 * 68, dtype=torch.uint8), 16, 2, 64)
+    b = lbm.KVBatch(torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 4, **i32), 2, 1)
+    z = lambda *shape: torch.zeros(*shape)
+    return [
+        (dict(q=z(2, 4, 64), k=z(2, 2, 64), v=z(2, 2, 64), q_out=z(2, 4, 64), cos=z(9, 32), sin=z(9, 32)), ["q_out"], [c.pages],
+         lambda q, k, v, q_out, cos, sin: lbm.lb_kv_append(c, b, q, k, v, rope=lbm.Rope(cos, sin), q_out=q_out)),
+        (dict(k_out=z(2, 2, 64), v_out=z(2, 2, 64)), ["k_out", "v_out"], [], lambda **t: lbm.lb_kv_read(c, b, **t)),
+        (dict(q=z(2, 4, 64), out=z(2, 4, 64), lse=z(2, 4)), ["out", "lse"], [], lambda q, out, lse: lbm.lb_kv_attend(c, b, q, 1.0, out=out, lse=lse)),
+        (dict(y=z(4, 16), x=z(4, 8), a=z(2, 8, 8), b=z(2, 16, 8), scale=z(2), out=z(4, 16)), ["out"], [],
+         lambda y, x, a, b, scale, out: lbm.lb_lora_add(y, x, a, b, z(4).int(), scale, out=out)),
+        (dict(y=z(4, 16), x=z(4, 8), a=z(2, 8, 8), b=z(2, 16, 8)), ["y"], [], lambda y, x, a, b: lbm.lb_lora_add(y, x, a, b, z(4).int())),
+        (dict(logits=z(4, 50), logprobs=z(4, 50), bias_values=z(1, 3)), ["logprobs"], [],
+         lambda logits, logprobs, bias_values: lbm.lb_logits_adjust(
+             logits, lbm.LogitRules(bias_ids=torch.zeros(1, 3, **i32), bias_values=bias_values), logprobs=logprobs)),
+    ]
+
+
+def test_binding_refuses_tensors_that_require_gradients(monkeypatch):
+    monkeypatch.setattr(scorer, "_call", lambda *a: None)
+    for tensors, _, _, call in small():
+        call(**tensors)
+        for name in tensors:
+            tensors[name].requires_grad_(True)
+            with pytest.raises(lbm.LBError, match=f"^LB_ERR_INVALID_ARG: {name} requires a gradient"):
+                call(**tensors)
+            with torch.no_grad():
+                call(**tensors)
+            tensors[name].requires_grad_(False)
+
+
+def test_binding_counts_what_it_writes_as_changed(monkeypatch):
+    """Torch's autograd refuses a backward pass over a saved tensor that was written since."""
+    monkeypatch.setattr(scorer, "_call", lambda *a: None)
+    for tensors, out, more, call in small():
+        before = {n: t._version for n, t in tensors.items()}
+        pages = [t._version for t in more]
+        call(**tensors)
+        for n, t in tensors.items():
+            assert (t._version > before[n]) == (n in out)
+        assert all(t._version > v for t, v in zip(more, pages))
+        with torch.inference_mode():
+            call(**{n: torch.zeros_like(t) for n, t in tensors.items()})
+    y, w = torch.ones(4, 16), torch.ones(4, 16, requires_grad=True)
+    loss = (y * w).sum()
+    lbm.lb_lora_add(y, torch.zeros(4, 8), torch.zeros(2, 8, 8), torch.zeros(2, 16, 8), torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
