@@ -124,6 +124,13 @@ def _elsewhere(g: int, **tensors) -> None:
             _bad(f"{name} is on {t.device}, the call's other tensors are on {f'cuda:{g}' if g >= 0 else 'cpu'}")
 
 
+def _counts(**values) -> None:
+    """Refuses the call for the first number that is negative or past 31 bits, of which ctypes would drop the rest."""
+    for name, n in values.items():
+        if n >> 31:
+            _bad(f"{name} must be in 0..2^31 - 1")
+
+
 def _no_gradient(**tensors) -> None:
     """Refuses the call for the first of its tensors that requires a gradient."""
     for name, t in tensors.items():
@@ -218,6 +225,8 @@ class KVCache:
         at = pages.shape
         if len(at) != 3 or at[1] != kv_heads or at[2] != page_tokens * (head_dim + head_dim // 16):
             _bad(f"pages has shape {tuple(at)}, expected (pages, {kv_heads}, {self.page_bytes(page_tokens, 1, head_dim)})")
+        if (page_tokens | kv_heads | head_dim) >> 31:
+            _counts(page_tokens=page_tokens, kv_heads=kv_heads, head_dim=head_dim)
         self.device = pages.get_device()
         if flags is not None and (flags.dtype is not torch.int32 or flags.numel() != 1 or flags.get_device() != self.device):
             _bad("flags must be one int32 on the pages' device")
@@ -260,6 +269,8 @@ class KVBatch:
             _ints(starts, "starts", (n + 1,))
             _ints(lengths, "lengths", (n,))
             _ints(pages, "the page table", (n, None))
+        if (n | n_rows | at[1] | max_new) >> 31:
+            _counts(n_seqs=n, n_rows=n_rows, max_pages=at[1], max_new=max_new)
         self.device = g = starts.get_device()
         if lengths.get_device() != g or pages.get_device() != g:
             _elsewhere(g, lengths=lengths, pages=pages)
@@ -280,6 +291,8 @@ class Rope:
         if cos.dtype is not torch.float32 or sin.dtype is not torch.float32 or cos.dim() != 2 or cos.shape != sin.shape \
                 or not cos.is_contiguous() or not sin.is_contiguous() or cos.device != sin.device:
             _bad("cos and sin must be contiguous float32 [positions, rot_dim / 2] on one device")
+        if (cos.shape[0] | 2 * cos.shape[1] | layout) >> 31:
+            _counts(positions=cos.shape[0], rot_dim=2 * cos.shape[1], layout=layout)
         self.cos, self.sin, self.device = cos, sin, cos.get_device()
         self.desc = lb_rope(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], layout, 0)
         self.ref = ctypes.addressof(self.desc)
@@ -325,6 +338,8 @@ class LogitRules:
             if mask_row.dtype is not i32 or len(mask_row.shape) != 1 or not mask_row.is_contiguous():
                 _ints(mask_row, "mask_row", (None,))
             mr = mask_row.data_ptr()
+        if (hw | bw | masks) >> 31:
+            _counts(history_width=hw, bias_width=bw, mask_rows=masks)
         self.desc = lb_logit_rules(temperature, repetition, presence, frequency, h, bi, bv, mk, mr, hw, bw, per_row, masks)
         self.ref = ctypes.addressof(self.desc)
 
@@ -336,7 +351,8 @@ def lb_rope_table(positions: int, rot_dim: int, base: float = 10000.0, scaling: 
                   trained: float = 0.0, low: float = 1.0, high: float = 4.0):
     """Host tables (cos, sin), float32 [positions, rot_dim / 2]."""
     _load()
-    cos = torch.empty((max(positions, 0), max(rot_dim, 0) // 2), dtype=torch.float32)
+    _counts(positions=positions, rot_dim=rot_dim, scaling=scaling)
+    cos = torch.empty((positions, rot_dim // 2), dtype=torch.float32)
     sin = torch.empty_like(cos)
     _lbm._check(_lbm.lib().lb_rope_table(positions, rot_dim, base, scaling, factor, trained, low, high, cos.data_ptr(),
                                          sin.data_ptr()))
@@ -402,6 +418,7 @@ def lb_kv_read(cache: KVCache, batch: KVBatch, dtype=None, k_out=None, v_out=Non
 
 
 def lb_kv_attend_workspace(cache: KVCache, batch: KVBatch, q_heads: int) -> int:
+    _counts(q_heads=q_heads)
     need = _L()
     _lbm._check((_lbm._lib or _lbm.lib()).lb_kv_attend_workspace(cache.ref, batch.ref, q_heads, ctypes.addressof(need)))
     return need.value
@@ -419,6 +436,8 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
     hq = q.shape[1]
     if batch.device != g or q.get_device() != g:
         _elsewhere(g, starts=batch.starts, q=q)
+    if (hq | window) >> 31:
+        _counts(q_heads=hq, window=window)
     written = () if out is None and lse is None else [t for t in (out, lse) if t is not None]
     if _recording() and (q.requires_grad or written):
         _no_gradient(q=q, out=out, lse=lse)
@@ -453,6 +472,7 @@ def lb_kv_attend(cache: KVCache, batch: KVBatch, q, scale: float, window: int = 
 @functools.lru_cache(maxsize=4096)
 def lb_lora_workspace(rows: int, d_in: int, d_out: int, rank: int) -> int:
     _load()
+    _counts(d_in=d_in, d_out=d_out, rank=rank)
     need = _L()
     _lbm._check((_lbm._lib or _lbm.lib()).lb_lora_workspace(rows, d_in, d_out, rank, ctypes.addressof(need)))
     return need.value
@@ -466,6 +486,8 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
     if x.dim() != 2 or y.dim() != 2 or a.dim() != 3 or b.dim() != 3:
         _bad("x and y must have 2 dimensions, a and b 3")
     (rows, d_out), d_in, (n, rank, _) = y.shape, x.shape[1], a.shape
+    if (d_in | d_out | rank | n) >> 31:
+        _counts(d_in=d_in, d_out=d_out, rank=rank, n_adapters=n)
     xs, ys = _rows(x, "x", rows, d_in, dtype), _rows(y, "y", rows, d_out, dtype)
     if out is None:
         out, os = y, ys
@@ -498,6 +520,7 @@ def lb_lora_add(y, x, a, b, adapter, scale=None, out=None, workspace=None, strea
 @functools.lru_cache(maxsize=4096)
 def lb_logits_workspace(rows: int, classes: int) -> int:
     _load()
+    _counts(classes=classes)
     need = _L()
     _lbm._check((_lbm._lib or _lbm.lib()).lb_logits_workspace(rows, classes, ctypes.addressof(need)))
     return need.value
@@ -512,6 +535,8 @@ def lb_logits_adjust(logits, rules: Optional[LogitRules] = None, target=None, wa
     if logits.dim() != 2:
         _bad("logits must have 2 dimensions")
     rows, classes = logits.shape
+    if classes >> 31:
+        _counts(classes=classes)
     stride = _rows(logits, "logits", rows, classes, logits.dtype)
     if _recording() and (logits.requires_grad or logprobs is not None or rules is not None):
         _no_gradient(logits=logits, logprobs=logprobs, bias_values=None if rules is None else rules.bias_values)

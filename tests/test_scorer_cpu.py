@@ -376,3 +376,32 @@ def test_binding_counts_what_it_writes_as_changed(monkeypatch):
     lbm.lb_lora_add(y, torch.zeros(4, 8), torch.zeros(2, 8, 8), torch.zeros(2, 16, 8), torch.zeros(4, dtype=torch.int32))
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_binding_refuses_numbers_past_32_bits(monkeypatch):
+    """ctypes would take them modulo 2^32.  Tensors of such sizes are on the meta device, without memory."""
+    monkeypatch.setattr(scorer, "_call", lambda *a: None)
+    big, i32 = 2 ** 32, dict(dtype=torch.int32)
+    c = lbm.KVCache(torch.zeros(3, 2, 16 * 68, dtype=torch.uint8), 16, 2, 64)
+    tables = torch.zeros(3, **i32), torch.zeros(2, **i32), torch.zeros(2, 4, **i32)
+    b = lbm.KVBatch(*tables, 2, 1)
+    meta = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="meta")
+    calls = [lambda: lbm.KVBatch(*tables, 2, big + 1), lambda: lbm.KVBatch(*tables, big + 2, 1), lambda: lbm.KVBatch(*tables, 2, -1),
+             lambda: lbm.KVBatch(meta(big + 3, **i32), meta(big + 2, **i32), meta(big + 2, 4, **i32), 2, 1),
+             lambda: lbm.KVBatch(tables[0], tables[1], meta(2, big + 4, **i32), 2, 1),
+             lambda: lbm.KVCache(meta(3, 2, (big + 16) * 68, dtype=torch.uint8), big + 16, 2, 64),
+             lambda: lbm.KVCache(meta(1, big + 2, 16 * 68, dtype=torch.uint8), 16, big + 2, 64),
+             lambda: lbm.Rope(meta(big + 8, 8), meta(big + 8, 8)), lambda: lbm.Rope(torch.zeros(4, 8), torch.zeros(4, 8), big),
+             lambda: lbm.LogitRules(history=meta(1, big + 2, **i32)), lambda: lbm.LogitRules(mask=meta(big + 1, 2, **i32)),
+             lambda: lbm.LogitRules(bias_ids=meta(1, big + 2, **i32), bias_values=meta(1, big + 2)),
+             lambda: lbm.lb_rope_table(big + 4, 16), lambda: lbm.lb_rope_table(4, big + 16), lambda: lbm.lb_rope_table(4, 16, 1e4, big),
+             lambda: lbm.lb_kv_attend_workspace(c, b, big + 2), lambda: lbm.lb_kv_attend(c, b, torch.zeros(2, 2, 64), 1.0, window=big),
+             lambda: lbm.lb_kv_attend(c, b, torch.zeros(2, 2, 64), 1.0, window=big + 5),
+             lambda: lbm.lb_lora_workspace(4, big + 8, 8, 8), lambda: lbm.lb_lora_workspace(4, 8, big + 8, 8), lambda: lbm.lb_lora_workspace(4, 8, 8, big + 8),
+             lambda: lbm.lb_lora_add(meta(1, 8), meta(1, big + 8), meta(1, 8, big + 8), meta(1, 8, 8), meta(1, **i32)),
+             lambda: lbm.lb_lora_add(meta(1, big + 8), meta(1, 8), meta(1, 8, 8), meta(1, big + 8, 8), meta(1, **i32)),
+             lambda: lbm.lb_logits_workspace(1, big + 41), lambda: lbm.lb_logits_adjust(meta(1, big + 41), target=meta(1, **i32))]
+    for k, call in enumerate(calls):
+        with pytest.raises(lbm.LBError, match=r"must be in 0\.\.2\^31 - 1"):
+            call()
+            print("not refused:", k)
