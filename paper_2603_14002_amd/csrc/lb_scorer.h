@@ -194,6 +194,13 @@ __device__ __forceinline__ void store8_nt(_Float16* p, const float (&x)[8]) {
   __builtin_nontemporal_store(w, reinterpret_cast<f16x8*>(p));
 }
 
+// x rounded to bf16, but finite if x is: the rest of it could not be taken from an infinity
+__device__ __forceinline__ __bf16 finite_bf16(float x) {
+  const __bf16 r = static_cast<__bf16>(x);
+  const uint32_t largest = 0x7F7F0000u | (__float_as_uint(x) & 0x80000000u);
+  return __builtin_isinf(static_cast<float>(r)) && !__builtin_isinf(x) ? static_cast<__bf16>(__uint_as_float(largest)) : r;
+}
+
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }

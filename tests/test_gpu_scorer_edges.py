@@ -255,3 +255,31 @@ def test_logits_of_long_rows_repeat_bit_for_bit(R, C, H, W, t):
         if first is None:
             first = logp, lse
         assert torch.equal(lse, first[1]) and torch.equal(logp, first[0])
+
+
+# ------------------------------------------------------------------ the largest numbers of a type
+
+
+def test_attend_queries_of_the_lowest_value():
+    """fp32 queries past bf16's largest number are finite: 0 times one is 0, and a small key's score is what 32 bits give."""
+    rng = np.random.default_rng(70)
+    low = torch.finfo(torch.float32).min
+    for new, length in ((1, 50), (1, 1500), (300, 320)):
+        say(f"[case] lowest queries {new} {length}")
+        R = ref.Ragged([new], [length], 16, 4, 64, seed=71)
+        k, v = randn(rng, length, 4, 64, dtype=torch.float64), randn(rng, length, 4, 64, dtype=torch.float64)
+        k[:, :, 3:5] = 0.0
+        k[:, 1, 32:] = 0.0
+        k[:, 1, 40] = torch.randint(0, 2, (length,)).double() * 2.0 ** -124  # scores 0 and about 2
+        R.put(0, k, v)
+        k, v = R.get(0, length)
+        q = randn(rng, new, 256, 64)
+        q[:, :, 3], q[:, :, 4] = low, -low
+        q[:, 64:128, 40] = -low
+        cache, batch = handles(R)
+        out, lse = lbm.lb_kv_attend(cache, batch, dev(q), 0.125, want_lse=True)
+        want, wl, _, reach = ref.attend(q.double(), k, v, 0.125, length - new, 0)
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+        b, bl = bounds(want, wl, *ref.attend(q.double(), k, v, 0.125, length - new, 0)[2:], torch.float32, 64, length)
+        close(out, want, b, "out")
+        close(lse, wl, bl, "lse")
