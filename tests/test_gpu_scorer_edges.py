@@ -283,3 +283,19 @@ def test_attend_queries_of_the_lowest_value():
         b, bl = bounds(want, wl, *ref.attend(q.double(), k, v, 0.125, length - new, 0)[2:], torch.float32, 64, length)
         close(out, want, b, "out")
         close(lse, wl, bl, "lse")
+
+
+@pytest.mark.parametrize("rank,rows,d_out", [(16, 3, 32), (32, 3, 32), (64, 20, 264), (128, 300, 40), (16, 300, 40)])
+def test_lora_products_past_the_largest_bf16(rank, rows, d_out):
+    """h = 2^128 - 2^118 is a finite 32-bit number that would round to an infinity in bf16: the result is 255.75 in each
+    channel, 256 in bf16, and its negative."""
+    say(f"[case] lora largest {rank} {rows}")
+    x = torch.zeros(rows, 64, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1] = 2.0 ** 127 * (2 - 2.0 ** -7), 1.5 * 2.0 ** 119
+    a = torch.zeros(2, rank, 64, dtype=torch.bfloat16)
+    a[0, 3, :2], a[1, rank - 1, :2] = 1.0, -1.0
+    b = torch.full((2, d_out, rank), 2.0 ** -120, dtype=torch.bfloat16)
+    y = torch.zeros(rows, d_out, dtype=torch.bfloat16)
+    ids = torch.arange(rows, dtype=torch.int32) % 2
+    out = lbm.lb_lora_add(*(dev(t) for t in (y, x, a, b, ids))).cpu().double()
+    assert torch.equal(out, torch.where(ids[:, None] == 0, 256.0, -256.0).double().expand_as(out))
