@@ -171,7 +171,9 @@ lb_status lb_kv_attend(const lb_kv_cache* cache, const lb_kv_batch* batch, int32
 /* out[i] = y[i] + scale[a] * B[a] (A[a] x[i]),  a = adapter[i]; rows whose
  * adapter is outside 0..n_adapters-1 become y[i].  Rows of one adapter need not
  * lie together (where they do, its weights are read once for all of them).
- * Products are summed in 32 bits and the sum is rounded once.
+ * Products are summed in 32 bits and the sum is rounded once; A x enters the
+ * product with B as it is for LB_F32, and to 2^-16 (LB_BF16) or 2^-21 (LB_F16) of
+ * its row's largest magnitude.
  *   x       device [rows][d_in], y, out device [rows][d_out], of `dtype`, with
  *           row strides; out may be y itself with the same stride, and may
  *           overlap x, where the workspace has 4 * rows * rank bytes at least
