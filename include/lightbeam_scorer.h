@@ -155,6 +155,8 @@ lb_status lb_kv_read(const lb_kv_cache* cache, const lb_kv_batch* batch, int32_t
  * infinities included, has no effect.  Scores, sums and outputs are held in 32
  * bits and an output is rounded once; the probabilities enter the products with
  * the values to 2^-16 of themselves for LB_BF16 and LB_F16, 2^-24 for LB_F32.
+ * Scores past 2^30 in magnitude, whose softmax is below their own rounding to 32
+ * bits, have no defined result.
  *   q, out     device [n_rows][q_heads][D] of `dtype`, row strides q_stride and
  *              out_stride (multiples of 16 B)
  *   lse        device float32 [n_rows][q_heads], or NULL
