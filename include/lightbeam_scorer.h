@@ -228,8 +228,9 @@ enum { LB_MAX_RULE_IDS = 4096 };
  *             target (padding), NaN for one >= classes
  *   lse       device float32 [rows]
  * (each may be NULL; target is read if score is not).  Masked classes get
- * -infinity whatever their logits hold, a row with nothing left -infinity
- * throughout.  rules NULL: none.
+ * -infinity whatever their logits hold, those whose z is -infinity whatever the
+ * rest of the row holds (else a row with a NaN is NaN), a row with nothing left
+ * -infinity throughout.  rules NULL: none.
  *   logits    device [rows][classes] of `dtype`, row stride logits_stride; rows at
  *             most 2^28, classes 2^30
  *   workspace  device, 16-B aligned, at least what lb_logits_workspace says for

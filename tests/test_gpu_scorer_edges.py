@@ -299,3 +299,135 @@ def test_lora_products_past_the_largest_bf16(rank, rows, d_out):
     ids = torch.arange(rows, dtype=torch.int32) % 2
     out = lbm.lb_lora_add(*(dev(t) for t in (y, x, a, b, ids))).cpu().double()
     assert torch.equal(out, torch.where(ids[:, None] == 0, 256.0, -256.0).double().expand_as(out))
+
+
+# ------------------------------------------------------------------ batches that do not fit
+
+
+FAULTS = {  # of two sequences of 2 new tokens, 20 and 30 in all, one of 4 rows
+    "none": {}, "page below": dict(page=-1), "page past": dict(page=6), "page far past": dict(page=2 ** 31 - 1), "page far below": dict(page=-2 ** 31),
+    "length past the table": dict(length=33), "length far past": dict(length=10 ** 9), "length below 0": dict(length=-1),
+    "length below the new tokens": dict(length=1), "length 0": dict(length=0), "starts past the rows": dict(starts=[0, 2, 9]),
+    "one sequence has all rows": dict(starts=[0, 4, 4]), "angles": dict(positions=29), "few angles": dict(positions=19), "max_new": dict(max_new=1),
+}
+
+
+@pytest.mark.parametrize("fault", list(FAULTS))
+@pytest.mark.parametrize("D,t", [(64, "f32"), (128, "bf16")])
+def test_append_and_attend_where_a_batch_does_not_fit(fault, D, t):
+    """Every byte of the pool after an append, and what attention gives after it, for the sequence that does not fit and
+    for the one that does."""
+    f = FAULTS[fault]
+    say(f"[case] faults {fault} {D}")
+    rng = np.random.default_rng(80)
+    R = ref.Ragged([2, 2], [20, 30], 16, 1, D, seed=6)
+    assert R.n_pages == 6
+    for s in range(2):
+        R.put(s, randn(rng, R.length[s], 1, D, dtype=torch.float64), randn(rng, R.length[s], 1, D, dtype=torch.float64))
+    k, v, q = (randn(rng, 4, 1, D, dtype=DT[t]) for _ in range(3))
+    if "page" in f:
+        R.table[0, 1] = f["page"]
+    if "length" in f:
+        R.lengths[0] = f["length"]
+    if "starts" in f:
+        R.starts[:] = torch.tensor(f["starts"], dtype=torch.int32)
+    max_new = f.get("max_new", 4 if "starts" in f else 2)
+    cache, batch = batch_of(R, max_new)
+    positions = f.get("positions", 40)
+    cos, sin = lbm.lb_rope_table(positions, 16)
+    rope = lbm.Rope(dev(cos), dev(sin))
+    # what the header says of it: (sequence, row, position) of the tokens there are, and the keys and values that go in
+    length = [min(max(int(x), 0), R.table.shape[1] * 16) for x in R.lengths]
+    rows = []
+    for s in range(2):
+        a, z = (min(max(int(x), 0), 4) for x in R.starts[s:s + 2])
+        rows += [(s, a + i, length[s] - (z - a) + i) for i in range(min(z - a, max_new))]
+    q_out = torch.full((4, 1, D), 7.0, dtype=DT[t], device="cuda:0")
+    lbm.lb_kv_append(cache, batch, dev(q), dev(k), dev(v), rope=rope, q_out=q_out)
+    pool = ref.Ragged([2, 2], [20, 30], 16, 1, D, seed=6)
+    pool.pages = R.pages.clone()
+    turned = set()
+    for s, row, p in rows:
+        if not 0 <= p < positions:
+            continue
+        turned.add(row)
+        page = int(R.table[s, p // 16])
+        if not 0 <= page < R.n_pages:
+            continue
+        pool.table = torch.full((1, p // 16 + 1), page, dtype=torch.int32)
+        kr = ref.rotate(k[row:row + 1].double(), cos[p:p + 1], sin[p:p + 1], False)
+        # put() writes from token 0 on: the one token goes in by way of a pool whose others are its own
+        tokens = [ref.Ragged.get(pool, 0, p + 1, pool.pages)[i] for i in range(2)]
+        before = pool.pages.clone()
+        pool.put(0, torch.cat([tokens[0][:p], kr]).nan_to_num(0), torch.cat([tokens[1][:p], v[row:row + 1].double()]).nan_to_num(0))
+        after = pool.pages
+        pool.pages = before
+        slot, P = p % 16, 16
+        at = torch.cat([slot * (D // 2) + torch.arange(D // 2), P * D // 2 + ((slot // 4) * (D // 2) + torch.arange(D // 2)) * 4 + slot % 4,
+                        P * D + slot * (D // 32) + torch.arange(D // 32),
+                        P * D + P * D // 32 + ((slot // 4) * (D // 32) + torch.arange(D // 32)) * 4 + slot % 4])
+        pool.pages[page][:, at] = after[page][:, at]
+    assert torch.equal(cache.pages.cpu(), pool.pages)
+    assert all(bool((q_out[i] == 7.0).all()) == (i not in turned) for i in range(4))
+    bits = 0
+    if "page" in f:
+        bits = lbm.LB_KV_BAD_PAGE
+    elif f and fault not in ("one sequence has all rows",):
+        bits = lbm.LB_KV_BAD_LENGTH
+    # (a length past the table is cut to the table, whose last entry here may be no page)
+    assert cache.status() & ~lbm.LB_KV_BAD_PAGE == bits & ~lbm.LB_KV_BAD_PAGE and cache.status() & bits == bits
+    cache.flags.zero_()
+    out, lse = torch.full((4, 1, D), 7.0, dtype=DT[t], device="cuda:0"), torch.full((4, 1), 7.0, device="cuda:0")
+    lbm.lb_kv_attend(cache, batch, dev(q), 0.3, out=out, lse=lse)
+    R.pages = pool.pages
+    for s, row, p in rows:
+        seen = [x for x in range(min(p, length[s] - 1) + 1) if 0 <= int(R.table[s, x // 16]) < R.n_pages]
+        if not seen:
+            assert bool((out[row] == 0).all()) and bool((lse[row] == -float("inf")).all())
+            continue
+        if any(x >= R.length[s] and (s, x) not in {(a, c) for a, _, c in rows} for x in seen):
+            continue  # of the pool's garbage, whose scales may be none that an append writes
+        pool.table = R.table[s:s + 1].clamp(0, R.n_pages - 1)
+        kk, vv = (x[seen] for x in ref.Ragged.get(pool, 0, max(seen) + 1, R.pages))
+        want, wl, mass, reach = ref.attend(q[row:row + 1].double(), kk, vv, 0.3, len(seen) - 1, 0)
+        b, bl = bounds(want, wl, mass, reach, DT[t], D, len(seen))
+        close(out[row:row + 1], want, b, f"row {row}")
+        close(lse[row:row + 1], wl, bl, f"lse of row {row}")
+    have = {row for _, row, _ in rows}
+    assert all(bool((out[i] == 7.0).all()) and bool((lse[i] == 7.0).all()) for i in range(4) if i not in have)
+
+
+@pytest.mark.parametrize("C", [41, 700, 30000])
+def test_logits_of_minus_infinity_beside_nan(C):
+    """A class without probability keeps -infinity where the rest of its row is NaN."""
+    x = torch.zeros(3, C)
+    x[0, 3], x[0, 7], x[1, 7], x[2, 3] = float("nan"), -float("inf"), -float("inf"), float("nan")
+    got, score, lse = lbm.lb_logits_adjust(dev(x), target=dev(torch.tensor([7, 7, 0], dtype=torch.int32)))
+    say(f"[case] logits -inf beside nan {C}")
+    assert got[0, 7] == -float("inf") and got[1, 7] == -float("inf") and score[0] == -float("inf") and score[1] == -float("inf")
+    assert int(torch.isnan(got[0]).sum()) == C - 1 and bool(torch.isnan(got[2]).all()) and bool(torch.isnan(score[2]))
+    assert torch.isnan(lse).tolist() == [True, False, True] and bool(torch.isfinite(got[1, :7]).all())
+
+
+def test_logits_with_the_longest_lists():
+    """4096 ids on the longest part of a row: as with the lists' last biases and counts put in by hand."""
+    say("[case] logits longest lists")
+    rng = np.random.default_rng(90)
+    C = 131072
+    for R in (1, 600):  # parts of a row, and a row in one
+        x = dev(randn(rng, R, C))
+        past, ids = (torch.from_numpy(rng.integers(0, C, (1, 2048)).astype(np.int32)) for _ in range(2))
+        values = randn(rng, 1, 2048)
+        on = lbm.LogitRules(history=dev(past.expand(R, -1).contiguous()), presence=0.5, frequency=0.25, bias_ids=dev(ids), bias_values=dev(values))
+        got, _, lse = lbm.lb_logits_adjust(x, on)
+        z = x.double()
+        counts = torch.bincount(past[0].long(), minlength=C).double()
+        bias = torch.zeros(C, dtype=torch.float64)
+        for w, b in zip(ids[0].tolist(), values[0].tolist()):
+            bias[w] = b
+        z += dev(bias - 0.5 * (counts > 0) - 0.25 * counts)
+        want = torch.logsumexp(z, 1)
+        # four roundings of the rules on values below 16, and sums of 2 C / 256 + 64 positive terms
+        bound = 6 * 2.0 ** -24 * 64 + (2 * C / 256 + 64) * 2.0 ** -24 + 2.0 ** -21 + 2.0 ** -22 * float(want.max())
+        close(lse, want.cpu(), bound, "lse")
+        close(got[0], (z - want[:, None])[0].cpu(), 2 * bound, "logprobs")
