@@ -151,7 +151,7 @@ lb_status lb_kv_read(const lb_kv_cache* cache, const lb_kv_batch* batch, int32_t
  * tokens t <= p, with window > 0 only those with t > p - window:
  *   out = sum_t softmax_t(scale * q . k_t) v_t,   lse = ln sum_t exp(scale * q . k_t)
  * Query head h reads KV head h / (q_heads / kv_heads).  A query that sees no
- * token gets out = 0 and lse = -infinity.  What unseen tokens hold, NaN and
+ * token, or has scores of -infinity alone, gets out = 0 and lse = -infinity.  What unseen tokens hold, NaN and
  * infinities included, has no effect.  Scores, sums and outputs are held in 32
  * bits and an output is rounded once; the probabilities enter the products with
  * the values to 2^-16 of themselves for LB_BF16 and LB_F16, 2^-24 for LB_F32.

@@ -447,8 +447,7 @@ struct Pieces<float> {
   static constexpr int q = 3, p = 3;
 };
 
-// large: some x may be infinite, which is one piece (the rest of it would be NaN), or
-// past bf16's largest number.
+// large: some x may be infinite or past bf16's largest number.
 template <bool large, int N>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&w)[N]) {
   float rest[8];
@@ -458,8 +457,8 @@ __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&w)[N]) {
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      w[k][i] = large && N > 1 ? finite_bf16(rest[i]) : static_cast<__bf16>(rest[i]);
-      if (k + 1 < N) rest[i] = large && __builtin_isinf(rest[i]) ? 0.0f : rest[i] - static_cast<float>(w[k][i]);
+      w[k][i] = large && N > 1 && k == 0 ? first_piece(rest[i]) : static_cast<__bf16>(rest[i]);
+      if (k + 1 < N) rest[i] = large && k > 0 && __builtin_isinf(rest[i]) ? 0.0f : rest[i] - static_cast<float>(w[k][i]);
     }
 }
 

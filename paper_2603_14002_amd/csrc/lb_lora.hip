@@ -188,13 +188,15 @@ struct Down {
         const bool second = paired && c * S::KS + j * S::W >= A.rank;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          T hi;
-          if constexpr (__is_same(T, __bf16))
-            hi = finite_bf16(x[c][i]);
-          else
+          T hi, lo;
+          if constexpr (__is_same(T, __bf16)) {
+            hi = first_piece(x[c][i]);
+            lo = static_cast<T>(x[c][i] - static_cast<float>(hi));
+          } else {
+            // an infinity is one piece: the rest of it would be NaN
             hi = static_cast<T>(x[c][i]);
-          // an infinity is one piece: the rest of it would be NaN
-          const T lo = __builtin_isinf(x[c][i]) ? T(0.0f) : static_cast<T>(x[c][i] - static_cast<float>(hi));
+            lo = __builtin_isinf(x[c][i]) ? T(0.0f) : static_cast<T>(x[c][i] - static_cast<float>(hi));
+          }
           v[0][c][i] = second ? lo : hi;
           if constexpr (pieces == 2) v[1][c][i] = lo;
         }

@@ -194,11 +194,11 @@ __device__ __forceinline__ void store8_nt(_Float16* p, const float (&x)[8]) {
   __builtin_nontemporal_store(w, reinterpret_cast<f16x8*>(p));
 }
 
-// x rounded to bf16, but finite if x is: the rest of it could not be taken from an infinity
-__device__ __forceinline__ __bf16 finite_bf16(float x) {
-  const __bf16 r = static_cast<__bf16>(x);
-  const uint32_t largest = 0x7F7F0000u | (__float_as_uint(x) & 0x80000000u);
-  return __builtin_isinf(static_cast<float>(r)) && !__builtin_isinf(x) ? static_cast<__bf16>(__uint_as_float(largest)) : r;
+// x rounded to bf16, but finite, so that the rest of it can be taken: that of an
+// infinity (NaN) is an infinity (NaN) then
+__device__ __forceinline__ __bf16 first_piece(float x) {
+  const float largest = __uint_as_float(0x7F7F0000u);
+  return static_cast<__bf16>(__builtin_amdgcn_fmed3f(x, -largest, largest));
 }
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {

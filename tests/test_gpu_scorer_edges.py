@@ -431,3 +431,28 @@ def test_logits_with_the_longest_lists():
         bound = 6 * 2.0 ** -24 * 64 + (2 * C / 256 + 64) * 2.0 ** -24 + 2.0 ** -21 + 2.0 ** -22 * float(want.max())
         close(lse, want.cpu(), bound, "lse")
         close(got[0], (z - want[:, None])[0].cpu(), 2 * bound, "logprobs")
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+def test_attend_infinite_queries(t):
+    """Scores of plus infinity make a row NaN, and so does a NaN; with minus infinity throughout a row is as one that
+    sees nothing.  No other row has any of it."""
+    inf = float("inf")
+    for new, length in ((1, 50), (1, 1500), (310, 320)):
+        say(f"[case] infinite queries {t} {new} {length}")
+        rng = np.random.default_rng(74)
+        R = ref.Ragged([new, 1], [length, 20], 16, 4, 64, seed=75)
+        k, v = randn(rng, length, 4, 64, dtype=torch.float64), randn(rng, length, 4, 64, dtype=torch.float64)
+        k[:, :, 2] = 1.0
+        R.put(0, k, v)
+        R.put(1, k[:20], v[:20])
+        q = randn(rng, new + 1, 256, 64, dtype=DT[t])
+        q[0, 0, 2], q[0, 64, 2], q[0, 128, 2] = inf, -inf, float("nan")  # heads 0, 64, 128: KV heads 0, 1, 2
+        cache, batch = handles(R)
+        out, lse = lbm.lb_kv_attend(cache, batch, dev(q), 0.125, want_lse=True)
+        assert bool(torch.isnan(out[0, 0]).all()) and bool(torch.isnan(out[0, 128]).all())
+        assert not bool(torch.isfinite(lse[0, [0, 64, 128]]).any())
+        assert bool((out[0, 64] == 0).all()) and lse[0, 64] == -inf
+        out[0, [0, 64, 128]] = 0.0
+        lse[0, [0, 64, 128]] = 0.0
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
