@@ -25,7 +25,8 @@
  * synchronises, so every call may be captured into a HIP graph; a workspace
  * belongs to one call at a time (two captured graphs that may run side by side
  * need one each) and holds nothing between calls.  Calls on different streams
- * may overlap if no memory that one of them writes is used by the other.
+ * may overlap if no memory that one of them writes is used by the other.  What a
+ * call writes overlaps nothing else of the call, except where that is said.
  * Descriptors are read during the call only.
  */
 #ifndef LIGHTBEAM_SCORER_H_

@@ -172,8 +172,9 @@ __device__ __forceinline__ uint32_t bytes_at(const uint32_t (&w)[4], int i) {
 // eight channels) items: queries, then keys, then values.  A lane has its
 // channels of all four tokens in flight, and the four lanes of a block of 32
 // channels agree on the scale by two quad moves.  24 000 tokens of 12 prompts, 32 + 16
-// heads of 128, bf16: 116 us, 4.5 TB/s; what the rows wait for (starts, lengths, page)
-// and the registers of the 64-bit rotation bound it.  Rows are read and written once,
+// heads of 128, bf16: 115 us, 4.5 TB/s; what the rows wait for (starts, lengths, page)
+// and the registers of the 64-bit rotation (four wavefronts a SIMD, three in fp32)
+// bound it.  Rows are read and written once,
 // past the caches (else 128 us).
 template <int D, typename T>
 __global__ __launch_bounds__(256) void k_append(AppendArgs A) {
@@ -973,7 +974,7 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend_short
 // Few query rows: a workgroup takes 16 rows and one part of their key range; its
 // four wavefronts take every fourth tile and join at the end.  once: nobody else
 // reads the keys, which then leave the caches to others (4 x 110 000 keys of 8 heads:
-// 89 us, else 99).
+// 92 us, else 100).
 template <int D, typename T, bool once>
 __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend(AttendArgs A) {
   constexpr int VC = D / 16;
@@ -1047,18 +1048,20 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend(Atten
 // from memory.  A ring of 2 A tiles has a barrier every A tiles: at step t the keys
 // of t + 1 and the values of t are read, made A steps or more before, and those of t
 // + 1 + A and t + A are made, in places that were last read A steps or more before.
-// Six prompts of 65..2048 tokens over 130..4096, 32 heads of 128 on 8, bf16: 341 us,
-// 680 TFLOP/s; vector instructions are issued in half of the SIMD cycles (a lane's
-// eight scores of a row take 8 products, exponentials and sums each), matrix ones run
-// in 29 %, and two wavefronts a SIMD do not cover each other's waits.
+// Six prompts of 65..2048 tokens over 130..4096, 32 heads of 128 on 8, bf16: 408 us,
+// 570 TFLOP/s; vector instructions are issued in 54 % of the SIMD cycles (a lane's
+// eight scores of a row take 8 products, exponentials and sums each, and 24 for their
+// two pieces), matrix ones run in 36 %, and two wavefronts a SIMD do not cover each
+// other's waits.
 template <int D>
 struct Shared {
   static constexpr int KC = D / 32, VC = D / 16;
-  static constexpr int A = D <= 128 ? 2 : 1, N = 2 * A;  // at most 64 KB: two workgroups a CU
+  static constexpr int A = D <= 128 ? 2 : 1, N = 2 * A;
   bf16x8 key[N][2 * KC][64], value[N][VC][64];  // [tile % N][half and channels, or channel][lane]
   uint32_t nan[N][2][64];
   int32_t any_nan[N];
 };
+static_assert(sizeof(Shared<64>) <= 80 << 10 && sizeof(Shared<128>) <= 80 << 10 && sizeof(Shared<256>) <= 80 << 10, "two workgroups a CU");
 
 template <int D>
 struct Maker {
@@ -1352,20 +1355,20 @@ constexpr int64_t kLeastGroups = 600;  // of 128 rows
 // How a call is cut up.  Sequences with at most few_rows query rows a KV head: tiles
 // of 16 rows, as many for each as max_new may need or, where those are more, numbered
 // by the rows there are (1024 single tokens beside a prompt of 500, 32 heads of 128 on
-// 8, bf16: 110 us, else 1462; two sequences of up to 100 new tokens: 8.0, else 7.6), and parts of the key range so that about three workgroups a CU exist
-// (as many as are resident with 128 channels in bf16: 4 x 110 000 keys of 8 heads
-// take 89 us with them, 102 with two, 92 with six, 97 with eight), each with 16 tiles of keys at
-// least; where there are many such jobs with at most 16 tiles of keys, a wavefront
-// takes one alone (1024 sequences of 3 to 256 keys, 4 heads of 64: 16 us, else 26).
-// The others: a workgroup takes the rows of its four wavefronts, and the workgroups
-// are numbered as append's units are, so that a ragged batch has no more than one
-// idle one a sequence and head.  A batch that may hold both gets both kernels, each
-// of which leaves the other's sequences alone.  The many-row kernel does an
-// eighth of the conversions, but it has no parts of keys: with fewer rows than fill
-// the chip (512 workgroups of 128 rows are resident) all goes to the other (8 KV heads
-// of 128 channels, 4 query heads each, bf16: 100 new tokens of 20 000, 25 groups of
-// 128 rows, 99 us, else 772; 1000 of 5000, 250 groups, 151 us, else 201; 3000 of 3000,
-// 750 groups, 170 us, else 127).
+// 8, bf16: 110 us, else 1462; two sequences of up to 100 new tokens: 8.0, else 7.6), and
+// parts of the key range so that about three workgroups a CU exist (as many as are
+// resident with 128 channels in bf16: 4 x 110 000 keys of 8 heads take 92 us with them,
+// 110 with two or eight, 100 with six), each with 16 tiles of keys at least; where there
+// are many such jobs with at most 16 tiles of keys, a wavefront takes one alone (1024
+// sequences of 3 to 256 keys, 4 heads of 64: 19 us, else 26).  The others: a workgroup
+// takes the rows of its four wavefronts, and the workgroups are numbered as append's
+// units are, so that a ragged batch has no more than one idle one a sequence and head.
+// A batch that may hold both gets both kernels, each of which leaves the other's
+// sequences alone.  The many-row kernel does an eighth of the conversions, but it has no
+// parts of keys: with fewer rows than fill the chip (512 workgroups of 128 rows are
+// resident) all goes to the other (8 KV heads of 128 channels, 4 query heads each, bf16:
+// 100 new tokens of 20 000, 25 groups of 128 rows, 110 us, else 907; 1000 of 5000, 250
+// groups, 175 us, else 237; 3000 of 3000, 750 groups, 191 us, else 148).
 AttendPlan attend_plan(const KvArgs& kv, int head_dim, int dtype) {
   AttendPlan p{};
   const int64_t G = kv.q_heads / kv.kv_heads, rows = kv.max_new * G;

@@ -7,11 +7,11 @@
 // classes that a history or a bias list names are few: they are left out of that
 // sweep, as the masked ones are, by one bit a class in LDS, and handled on their
 // own from a hash table of at most LB_MAX_RULE_IDS entries, so the sweep has no
-// branch for them.  4096 rows of 125 002 in bf16, scores alone: 190 us, 5.4 TB/s,
+// branch for them.  4096 rows of 125 002 in bf16, scores alone: 192 us, 5.3 TB/s,
 // bound by memory (205 us where what is read once stays in the caches).
 //
 // Short rows (up to 512 classes): 16 or 64 lanes hold a row in registers and
-// read it once, the next one on its way.  128 000 rows of 41 in fp32: 14.5 us, 2.9
+// read it once, the next one on its way.  128 000 rows of 41 in fp32: 14.2 us, 3.0
 // TB/s, bound by the two reductions of a row, each four dependent steps.
 #include <hip/hip_runtime.h>
 

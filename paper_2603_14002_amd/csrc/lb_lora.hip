@@ -208,7 +208,7 @@ struct Down {
 // out = y + s B h.  whole: h is computed here too, by each workgroup for its own
 // channels, else k_lora_down has left it in the workspace.  8192 x 6144 in bf16, rank
 // 16: 44 us, 4.5 TB/s (a plain elementwise kernel: 36); 128 rows of their own adapters,
-// rank 64, 8192 channels: 30 us, 4.5 TB/s of weights.  Bound by memory.
+// rank 64, 8192 channels: 30 us, 4.0 TB/s of weights.  Bound by memory.
 template <typename T, int RT, bool whole>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs A) {
   using S = Step<T>;
