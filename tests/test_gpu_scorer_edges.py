@@ -456,3 +456,39 @@ def test_attend_infinite_queries(t):
         out[0, [0, 64, 128]] = 0.0
         lse[0, [0, 64, 128]] = 0.0
         assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("long", [40, 1500])
+def test_attend_loose_batches_captured_and_replayed(long):
+    """A graph captured under a bound serves other sequences of the same tensors: each replay is the eager call."""
+    say(f"[case] loose graph {long}")
+    rng = np.random.default_rng(46)
+    S = 30
+    R = filled(ref.Ragged([1] * S, [20] * (S - 2) + [long, long], 16, 2, 64, seed=47, pad_rows=50), rng)
+    cache, batch = batch_of(R, 64)
+    q = dev(randn(rng, R.n_rows, 4, 64))
+    ws = torch.empty(max(16, lbm.lb_kv_attend_workspace(cache, batch, 4)), dtype=torch.uint8, device="cuda:0")
+    out, lse = torch.zeros(R.n_rows, 4, 64, device="cuda:0"), torch.zeros(R.n_rows, 4, device="cuda:0")
+    step = lambda: lbm.lb_kv_attend(cache, batch, q, 0.2, out=out, lse=lse, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for new in ([1] * S, [0] * (S - 1) + [39], [2] * 20 + [0] * 9 + [19], [20] + [0] * 10 + [1] * 18 + [30], [0] * S):
+        batch.starts.copy_(dev(torch.tensor(np.cumsum([0] + new).astype(np.int32))))
+        results = []
+        for run in (g.replay, step):
+            out.fill_(7.0), lse.fill_(7.0)
+            run()
+            torch.cuda.synchronize()
+            results.append((out.clone(), lse.clone()))
+        for a, b in zip(*results):
+            assert torch.equal(a, b) and bool((a[sum(new):] == 7.0).all())
+        R.new = new
+        check_some(R, q, *results[0], 0.2, 0, [s for s in range(S) if new[s]])
+    assert cache.status() == 0
