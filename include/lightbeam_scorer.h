@@ -152,12 +152,12 @@ lb_status lb_kv_read(const lb_kv_cache* cache, const lb_kv_batch* batch, int32_t
  * tokens t <= p, with window > 0 only those with t > p - window:
  *   out = sum_t softmax_t(scale * q . k_t) v_t,   lse = ln sum_t exp(scale * q . k_t)
  * Query head h reads KV head h / (q_heads / kv_heads).  A query that sees no
- * token, or has scores of -infinity alone, gets out = 0 and lse = -infinity.  What unseen tokens hold, NaN and
- * infinities included, has no effect.  Scores, sums and outputs are held in 32
- * bits and an output is rounded once; the probabilities enter the products with
- * the values to 2^-16 of themselves for LB_BF16 and LB_F16, 2^-24 for LB_F32.
- * Scores past 2^30 in magnitude, whose softmax is below their own rounding to 32
- * bits, have no defined result.
+ * token, or has scores of -infinity alone, gets out = 0 and lse = -infinity.
+ * What unseen tokens hold, NaN and infinities included, has no effect.  Scores,
+ * sums and outputs are held in 32 bits and an output is rounded once; the
+ * probabilities enter the products with the values to 2^-16 of themselves for
+ * LB_BF16 and LB_F16, 2^-24 for LB_F32.  Scores past 2^30 in magnitude, whose
+ * softmax is below their own rounding to 32 bits, have no defined result.
  *   q, out     device [n_rows][q_heads][D] of `dtype`, row strides q_stride and
  *              out_stride (multiples of 16 B)
  *   lse        device float32 [n_rows][q_heads], or NULL
@@ -236,8 +236,8 @@ enum { LB_MAX_RULE_IDS = 4096 };
  *             most 2^28, classes 2^30
  *   workspace  device, 16-B aligned, at least what lb_logits_workspace says for
  *              these rows and classes (NULL if that is 0)
- * A call made again gives the same bits.  logits is only read; logprobs may be the logits themselves where these are
- * LB_F32 with the same stride. */
+ * A call made again gives the same bits.  logits is only read; logprobs may be
+ * the logits themselves where these are LB_F32 with the same stride. */
 lb_status lb_logits_workspace(int64_t rows, int32_t classes, int64_t* bytes);
 lb_status lb_logits_adjust(int32_t dtype, int64_t rows, int32_t classes, const void* logits,
                            int64_t logits_stride, const lb_logit_rules* rules, const int32_t* target,

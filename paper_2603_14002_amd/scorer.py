@@ -70,8 +70,8 @@ def declare(L) -> None:
 
 
 # torch, this package, torch's current raw stream of a device, its current device, whether it records gradients
-# and what counts a tensor as changed, set by _load() before the first use: the package can be imported without torch, and a call of a few microseconds has no time for
-# an import statement in each helper
+# and what counts a tensor as changed, set by _load() before the first use: the package can be imported without
+# torch, and a call of a few microseconds has no time for an import statement in each helper
 torch = _lbm = _raw_stream = _current_device = _recording = _changed = None
 _DTYPE = {}
 
