@@ -149,7 +149,8 @@ lb_status lb_kv_read(const lb_kv_cache* cache, const lb_kv_batch* batch, int32_t
 
 /* Attention of a batch's new tokens over their sequences' cached tokens (their
  * own included: append first).  The query of a token at position p sees the
- * tokens t <= p, with window > 0 only those with t > p - window:
+ * tokens t <= p, with window > 0 only those with t > p - window (pages of which no
+ * query sees a token need not be there):
  *   out = sum_t softmax_t(scale * q . k_t) v_t,   lse = ln sum_t exp(scale * q . k_t)
  * Query head h reads KV head h / (q_heads / kv_heads).  A query that sees no
  * token, or has scores of -infinity alone, gets out = 0 and lse = -infinity.

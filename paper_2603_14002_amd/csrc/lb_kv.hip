@@ -500,25 +500,26 @@ __device__ __forceinline__ uint32_t carry_255(uint32_t w) { return (w & 0x7F7F7F
 // The pages of a key range: tiles of 32 tokens from `begin` on, of which a
 // wavefront takes every `step`-th.  Lane i holds the pages (of both halves of 16
 // tokens) of the i-th of the next 64 tiles, so a tile's address needs no load
-// before it.
+// before it.  Halves that end before `first`, which nobody sees, have none.
 struct Pages {
   const int32_t* table;
-  int32_t n_pages, shift, begin, end, step;
+  int32_t n_pages, shift, begin, first, end, step;
   static constexpr int32_t kNothing = -(1 << 29);  // no tile is within 64 steps of it
   int32_t held, page0, page1;
 
-  __device__ __forceinline__ Pages(const KvArgs& A, int32_t s, int32_t begin_, int32_t end_, int32_t step_)
+  __device__ __forceinline__ Pages(const KvArgs& A, int32_t s, int32_t first_, int32_t end_, int32_t step_)
       : table(A.table + static_cast<int64_t>(s) * A.max_pages), n_pages(static_cast<int32_t>(A.n_pages)), shift(A.page_shift),
-        begin(begin_), end(end_), step(step_), held(kNothing), page0(-1), page1(-1) {}
+        begin(first_ & ~31), first(first_), end(end_), step(step_), held(kNothing), page0(-1), page1(-1) {}
 
   // makes lane i hold the pages of tile t + i * step
   __device__ __forceinline__ void hold(int32_t t, uint32_t* flags) {
     const int lane = threadIdx.x & 63;
     held = t;
     const int64_t tok = begin + (static_cast<int64_t>(t) + static_cast<int64_t>(lane) * step) * 32;
-    page0 = tok < end ? table[tok >> shift] : -1;
-    page1 = tok + 16 < end ? table[(tok + 16) >> shift] : -1;
-    if ((tok < end && (page0 < 0 || page0 >= n_pages)) || (tok + 16 < end && (page1 < 0 || page1 >= n_pages))) {
+    const bool seen0 = tok < end && tok + 16 > first, seen1 = tok + 16 < end && tok + 32 > first;
+    page0 = seen0 ? table[tok >> shift] : -1;
+    page1 = seen1 ? table[(tok + 16) >> shift] : -1;
+    if ((seen0 && (page0 < 0 || page0 >= n_pages)) || (seen1 && (page1 < 0 || page1 >= n_pages))) {
       raise(flags, LB_KV_BAD_PAGE);
       if (page0 >= n_pages) page0 = -1;
       if (page1 >= n_pages) page1 = -1;
@@ -581,8 +582,8 @@ struct Keys {
   int64_t page_bytes;
   uint32_t k_at, v_at, ks_at, vs_at;
 
-  __device__ __forceinline__ Keys(const KvArgs& A, int32_t s, int32_t h, int32_t begin, int32_t end, int32_t step, int n, int j)
-      : P(A, s, begin, end, step) {
+  __device__ __forceinline__ Keys(const KvArgs& A, int32_t s, int32_t h, int32_t first, int32_t end, int32_t step, int n, int j)
+      : P(A, s, first, end, step) {
     const int32_t T = 1 << A.page_shift, block = T * (D + D / 16);
     base = A.pages + static_cast<int64_t>(h) * block;
     page_bytes = static_cast<int64_t>(block) * A.kv_heads;
@@ -676,7 +677,7 @@ struct Rows {
   float m[QT], l[QT];  // reference and the lane's share of the sum of exp2(score - reference)
   int32_t pos[QT];     // the lane's row's position, -1: no row
   float scale2;        // log2(e) |scale|, its sign is in q
-  int32_t window, end, p_min, p_max;  // p_min, p_max: over the rows there are
+  int32_t window, first, end, p_min, p_max;  // over the rows there are: tokens first .. end - 1 are seen by some
 
   // How far a score may pass the reference before the reference moves: sums of
   // exp2 keep their precision, and most tiles need no exchange between lanes.
@@ -888,6 +889,7 @@ __device__ __forceinline__ bool rows_of(const AttendArgs& A, const Job& w, int32
   const bool have = r0 < w.R;
   S.p_min = have ? w.q.pos0 + r0 / w.G : -1;
   S.p_max = have ? w.q.pos0 + (min(w.R, r0 + 16 * QT) - 1) / w.G : -1;
+  S.first = A.window > 0 ? max(0, S.p_min - A.window + 1) : 0;
   S.end = min(w.q.len, S.p_max + 1);
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -965,9 +967,8 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend_short
   if (lane == 0) report(A, w, job);
   Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
-  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
-  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 1, n, j);
-  S.template sweep<false>(K, 0, S.end > begin ? (S.end - begin + 31) >> 5 : 0, j, A.kv.flags);
+  Keys<D> K(A.kv, w.s, w.h, S.first, S.end, 1, n, j);
+  S.template sweep<false>(K, 0, S.end > K.P.begin ? (S.end - K.P.begin + 31) >> 5 : 0, j, A.kv.flags);
   store_rows<D, T, 1>(A, w, w.tile * 16, S, n, j);
 }
 
@@ -985,10 +986,9 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, 1)) void k_attend(Atten
   if (split == 0 && threadIdx.x == 0) report(A, w, job);
   Rows<D, T, 1> S;
   if (!rows_of<D, T, 1>(A, w, w.tile * 16, S, n, j)) return;
-  const int32_t begin = A.window > 0 ? max(0, S.p_min - A.window + 1) & ~31 : 0;
-  const int32_t tiles = S.end > begin ? (S.end - begin + 31) >> 5 : 0;
+  Keys<D> K(A.kv, w.s, w.h, S.first, S.end, 4, n, j);
+  const int32_t tiles = S.end > K.P.begin ? (S.end - K.P.begin + 31) >> 5 : 0;
   const int32_t per = (tiles + A.splits - 1) / A.splits;
-  Keys<D> K(A.kv, w.s, w.h, begin, S.end, 4, n, j);
   S.template sweep<once>(K, split * per + wave, min(tiles, (split + 1) * per), j, A.kv.flags);
   const float l = row_sum(S.l[0]);
 
@@ -1077,8 +1077,8 @@ struct Maker {
   const uint8_t* scales[2];
   int there = 0;             // the halves there are of that tile
 
-  __device__ __forceinline__ Maker(const KvArgs& A, int32_t s, int32_t h, int32_t begin, int32_t end, int wave, int n, int j)
-      : P(A, s, begin, end, 1), u(wave >> 1), ks(0), ok(0) {
+  __device__ __forceinline__ Maker(const KvArgs& A, int32_t s, int32_t h, int32_t first, int32_t end, int wave, int n, int j)
+      : P(A, s, first, end, 1), u(wave >> 1), ks(0), ok(0) {
     const int32_t T = 1 << A.page_shift, block = T * (D + D / 16), c0 = (wave & 1) * F, w0 = D == 64 ? wave >> 1 : wave * W;
     base = A.pages + static_cast<int64_t>(h) * block;
     page_bytes = static_cast<int64_t>(block) * A.kv_heads;
@@ -1172,11 +1172,11 @@ __global__ __launch_bounds__(256, waves(D, Pieces<T>::q, QT)) void k_attend_rows
   Rows<D, T, QT> S;
   const bool have = rows_of<D, T, QT>(A, w, (w.tile * 4 + wave) * 16 * QT, S, n, j);
   // the key range of all four wavefronts' rows
-  const int32_t first = w.q.pos0 + w.tile * per / w.G, last = w.q.pos0 + (min(w.R, (w.tile + 1) * per) - 1) / w.G;
-  const int32_t begin = A.window > 0 ? max(0, first - A.window + 1) & ~31 : 0, end = min(w.q.len, last + 1);
+  const int32_t p_min = w.q.pos0 + w.tile * per / w.G, p_max = w.q.pos0 + (min(w.R, (w.tile + 1) * per) - 1) / w.G;
+  const int32_t first = A.window > 0 ? max(0, p_min - A.window + 1) : 0, begin = first & ~31, end = min(w.q.len, p_max + 1);
   const int32_t tiles = end > begin ? (end - begin + 31) >> 5 : 0;
   if (tiles > 0) {
-    Maker<D> M(A.kv, w.s, w.h, begin, end, wave, n, j);
+    Maker<D> M(A.kv, w.s, w.h, first, end, wave, n, j);
     f32x4 acc[QT][2];
     bf16x8 kf[KA], vf[VA];
     const auto read_keys = [&](int b) {

@@ -492,3 +492,49 @@ def test_attend_loose_batches_captured_and_replayed(long):
         R.new = new
         check_some(R, q, *results[0], 0.2, 0, [s for s in range(S) if new[s]])
     assert cache.status() == 0
+
+
+# ------------------------------------------------------------------ what lies before a window
+
+WINDOWED = [  # new, length, page, q heads, kv heads, D, window, type: each of the kernels, and parts of the keys
+    ([1, 1], [300, 77], 16, 4, 2, 64, 50, "f32"),
+    ([1], [5000], 16, 4, 1, 128, 2100, "bf16"),
+    ([3, 1], [200, 450], 32, 2, 1, 256, 33, "f16"),
+    ([1] * 530, [100 + i % 300 for i in range(530)], 16, 4, 4, 64, 20, "bf16"),
+    ([650], [900], 16, 128, 8, 64, 70, "bf16"),
+    ([310, 300], [630, 433], 16, 128, 4, 128, 90, "f32"),
+    ([305], [506], 32, 256, 2, 256, 100, "bf16"),
+]
+
+
+def windowed(case):
+    """The case's tensors, and the first position of each sequence that some new token sees."""
+    new, length, P, Hq, H, D, window, t = WINDOWED[case]
+    rng = np.random.default_rng(600 + case)
+    R = filled(ref.Ragged(new, length, P, H, D, seed=case), rng, shared=len(new) > 100)
+    first = [max(0, ln - n - window + 1) for n, ln in zip(new, length)]
+    return R, dev(randn(rng, R.n_rows, Hq, D, dtype=DT[t])), D ** -0.5, window, first
+
+
+@pytest.mark.parametrize("case", range(len(WINDOWED)))
+def test_attend_pages_before_the_window_may_be_gone(case):
+    """A page of which no query sees a token need not be one, and is no fault of the data."""
+    say(f"[case] window gone {case}")
+    R, q, scale, window, first = windowed(case)
+    cache, batch = handles(R)
+    want = lbm.lb_kv_attend(cache, batch, q, scale, window=window, want_lse=True)
+    assert cache.status() == 0
+    for s, f in enumerate(first):
+        R.table[s, :f // R.P] = -1 if s % 2 else R.n_pages + 7
+    cache, batch = handles(R)
+    got = lbm.lb_kv_attend(cache, batch, q, scale, window=window, want_lse=True)
+    assert cache.status() == 0
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    # a page that is seen in its last token alone is needed
+    s = len(first) - 1
+    if first[s]:
+        R.table[s, first[s] // R.P] = -1
+        cache, batch = handles(R)
+        lbm.lb_kv_attend(cache, batch, q, scale, window=window)
+        assert cache.status() == lbm.LB_KV_BAD_PAGE
