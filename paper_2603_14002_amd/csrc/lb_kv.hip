@@ -620,21 +620,22 @@ struct Keys {
 // gfx950), so the other bytes need not be cleared.
 __device__ __forceinline__ float scale_at(uint32_t word, int i) { return __uint_as_float(i == 3 ? word >> 1 : word << (23 - 8 * i)); }
 
-// The values' scales of a tile; tokens from `end` on, and of halves that do not
-// exist, get the byte 0, whatever the cache holds there, and so do blocks of NaN:
-// which these are is left in `nan`, 255 a byte.
+// The values' scales of a tile; tokens before `first` and from `end` on, and of halves
+// that do not exist, get the byte 0, whatever the cache holds there (0 times an infinity
+// would be NaN), and so do blocks of NaN: which these are is left in `nan`, 255 a byte.
 struct ValueScales {
   uint32_t bytes[2], nan[2];
   bool any_nan;  // in some lane
 
-  __device__ __forceinline__ ValueScales(const uint32_t (&vs)[2], bool whole, int32_t tb, int32_t end, int ok, int j) {
+  __device__ __forceinline__ ValueScales(const uint32_t (&vs)[2], int32_t tb, int32_t first, int32_t end, int ok, int j) {
     bytes[0] = vs[0], bytes[1] = vs[1];
-    if (!whole) {
+    if (ok != 3 || tb < first || tb + 32 > end) {
       const int32_t at = behind_branch(tb);  // most tiles are whole
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int32_t left = ok >> u & 1 ? end - (at + 16 * u + 4 * j) : 0;
+        const int32_t tok = at + 16 * u + 4 * j, left = ok >> u & 1 ? end - tok : 0, before = first - tok;
         bytes[u] = left >= 4 ? bytes[u] : left <= 0 ? 0u : bytes[u] & ((1u << (8 * left)) - 1u);
+        bytes[u] = before <= 0 ? bytes[u] : before >= 4 ? 0u : bytes[u] >> (8 * before) << (8 * before);
       }
     }
     nan[0] = nan[1] = 0;
@@ -773,7 +774,7 @@ struct Rows {
         },
         acc);
     weigh(acc, tb, ok, j, pf);
-    const ValueScales V(X.vs, ok == 3 && tb + 32 <= end, tb, end, ok, j);
+    const ValueScales V(X.vs, tb, first, end, ok, j);
 #pragma unroll
     for (int w = 0; w < D / 32; ++w) {
       uint32_t y[2][4];
@@ -1125,7 +1126,7 @@ struct Maker {
     for (int i = 0; i < F; ++i) L.key[b][wave * F + i][lane] = bf16_of(k[i], s);
   }
   __device__ __forceinline__ void make_values(Shared<D>& L, int b, int32_t tb, int wave, int lane) const {
-    const ValueScales V(vs, ok == 3 && tb + 32 <= P.end, tb, P.end, ok, lane >> 4);
+    const ValueScales V(vs, tb, P.first, P.end, ok, lane >> 4);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       uint32_t y[2][4];

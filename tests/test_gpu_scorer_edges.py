@@ -538,3 +538,25 @@ def test_attend_pages_before_the_window_may_be_gone(case):
         cache, batch = handles(R)
         lbm.lb_kv_attend(cache, batch, q, scale, window=window)
         assert cache.status() == lbm.LB_KV_BAD_PAGE
+
+
+@pytest.mark.parametrize("case", range(len(WINDOWED)))
+def test_attend_tokens_before_the_window_have_no_effect(case):
+    """Whatever bytes they hold, scales that stand for no number among them."""
+    say(f"[case] window bytes {case}")
+    R, q, scale, window, first = windowed(case)
+    cache, batch = handles(R)
+    want = lbm.lb_kv_attend(cache, batch, q, scale, window=window, want_lse=True)
+    P, D = R.P, R.D
+    for byte in (253, 254, 255):
+        for s, f in enumerate(first):
+            for x in range(max(0, f - 40), f):
+                mem, slot = R.pages[int(R.table[s, x // P])], x % P
+                mem[:, slot * (D // 2):(slot + 1) * (D // 2)] = 0x77
+                mem[:, P * D // 2 + ((slot // 4) * (D // 2) + torch.arange(D // 2)) * 4 + slot % 4] = 0x77
+                mem[:, P * D + slot * (D // 32):P * D + (slot + 1) * (D // 32)] = byte
+                mem[:, P * D + P * D // 32 + ((slot // 4) * (D // 32) + torch.arange(D // 32)) * 4 + slot % 4] = byte
+        cache, batch = handles(R)
+        got = lbm.lb_kv_attend(cache, batch, q, scale, window=window, want_lse=True)
+        for a, b in zip(want, got):
+            assert torch.equal(a, b), byte
